@@ -49,6 +49,8 @@ extern "C" {
 #define EARN_F32 0
 #define EARN_BF16 1
 
+/* Longest cache the calls over pages take. */
+#define EARN_MAX_CACHE_LEN (1 << 30)
 /* Largest number of tensors one earn_compact_registers call gathers. */
 #define EARN_MAX_COMPACT_TENSORS 112
 
@@ -402,6 +404,103 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
                            const int32_t* stream_to_seq, void* gen_k, void* gen_v, const int32_t* gen_len,
                            const int32_t* gen_src, int32_t gen_cap, int32_t n_streams, int32_t batch,
                            int32_t max_shared_len, int32_t shared_total, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Caches in pages: serving streams one token at a time without a contiguous cache for each (the cache of paper Section 2.2,
+ * Eq. 4, at any length; beams and register caches as elsewhere in this file need none of this).
+ *
+ * A pool holds pages of page_size rows, k_pages and v_pages [n_pages, Hkv, page_size, d]: the rows of one kv head lie side by
+ * side.  Row r of stream u (0 <= r < max_pages * page_size) is row r % page_size of page page_table[u][r / page_size]; the
+ * table is [n_streams, max_pages] int32, device.  Several streams may name the same page as long as no call writes to it.
+ * Any page_size > 0.  A table entry outside [0, n_pages) names no page: rows there are not attended (they weigh 0), what would
+ * be stored there is dropped.  Lengths beyond what a table holds, or beyond the bound passed by value, are cut back to it.  So no
+ * value in device memory leads outside the pools; wrong values give wrong results.  A negative cache_len marks an idle stream
+ * (a place of a padded batch): nothing of it is read or stored but zeros in its rows of `out`.
+ * earn_set_validation(1) adds: table entries of rows in use inside the pool, lengths within their bounds, pages that a call
+ * writes named once and by no other stream, positions in [0, 2^24).
+ *
+ * earn_cache_store: the rows of a prefill go to their pages.  Row i of packed sequence s (stream s of the table) becomes row
+ * start[s] + i.  A pure copy: hand over k_rot_out of the prefill or k_out of the projection, keys are stored as they are.
+ *   k, v        [total_tokens, Hkv, d]                cu_seqlens  [batch+1] int32, device
+ *   start       [batch] int32, device, or NULL (0): rows that are in the pages already
+ * desc: dtype, n_kv_heads and head_dim are used.  total_tokens == 0 is a no-op.
+ *
+ * earn_decode_attn_paged: one decode step.  With n = cache_len[u]:
+ *   q' = RoPE(q_u, q_pos[u]);  k' = RoPE(k_new_u, q_pos[u]), rounded to the cache's type;  row n of the stream := (k', v_new_u)
+ *   out_u = softmax over rows 0 .. n of (q' . key * scale), times values
+ * A position is not a row number: caches that rows were evicted from go on at their streams' own positions.  A new row without
+ * a place (no page, or n at the table's end) is attended but not stored.
+ *   q           [n_streams, Hq, d]                     k_new, v_new  [n_streams, Hkv, d], k_new not yet rotated
+ *   q_pos, cache_len  [n_streams] int32, device        max_cache_len  upper bound on cache_len
+ *   weights_out [n_streams, Hkv, weight_rows] fp32 or NULL: running sums of the softmax weights, per kv head over its query heads:
+ *               weights_out[u][c][r] = weights_in[u][c][r] + sum_a p_a(r)   for r < n, and without weights_in for r = n (a new
+ *               row's sum starts here); rows behind n are left as they are, rows from weight_rows on have no sum
+ *   weights_in  the same layout, or NULL (zeros); may be weights_out itself
+ *   out         [n_streams, Hq, d]
+ *   workspace   at least earn_decode_paged_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0
+ * Errors: as earn_decode_attn; more than 128 query heads per kv head -> UNSUPPORTED.  Long caches are split over workgroups and joined in
+ * a second launch.
+ *
+ * earn_cache_evict: streams that have outgrown `budget` keep, for every kv head on its own, rows [0, n_first), rows [n - n_last,
+ * n) and of the rows between them the budget - n_first - n_last with the largest weights (equal ones: the lower row; NaN counts
+ * as less than anything; n = cache_len[u]).  The kept rows move in their order to rows 0, 1, ... of the pages that new_table
+ * names; a stream of at most `budget` rows moves whole.  The old pages and weights are only read: the caller goes on with
+ * new_table, len_out and weights_out and may then use the old pages for other streams.
+ *   weights     [n_streams, Hkv, weight_rows] fp32 (weights_out of the decode steps); cache_len <= weight_rows
+ *   new_table   [n_streams, new_max_pages] int32, device: pages of the same pools that no stream of the call reads from, each
+ *               named once; new_max_pages * page_size >= budget
+ *   kept_out    [n_streams, Hkv, budget] int32: the old row of every kept one, -1 behind the last
+ *   len_out     [n_streams] int32: min(cache_len, budget), an idle stream's -1; may be cache_len itself
+ *   weights_out [n_streams, Hkv, weight_rows_out] fp32 or NULL: the kept rows' sums; must not overlap `weights`;
+ *               weight_rows_out >= budget; rows behind the last are left as they are
+ *   workspace   at least earn_cache_evict_workspace_bytes(...) bytes; may be NULL when that is 0
+ * Errors: NULL required pointer, non-positive size, n_first or n_last < 0, n_first + n_last > budget, a bound that does not hold
+ * -> INVALID_ARG; desc as for earn_prefill_attn (dtype, n_kv_heads, head_dim are used).
+ */
+int earn_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* start,
+                     int32_t batch, int32_t total_tokens, void* k_pages, void* v_pages, const int32_t* page_table,
+                     int32_t max_pages, int32_t n_pages, int32_t page_size, void* stream);
+int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new,
+                           const int32_t* q_pos, void* k_pages, void* v_pages, const int32_t* page_table,
+                           const int32_t* cache_len, int32_t n_streams, int32_t max_pages, int32_t n_pages,
+                           int32_t page_size, int32_t max_cache_len, const float* weights_in, float* weights_out,
+                           int32_t weight_rows, void* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t earn_decode_paged_workspace_bytes(const earn_attn_desc* desc, int32_t n_streams, int32_t max_cache_len,
+                                         int32_t have_weights);
+int earn_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, const int32_t* page_table,
+                     const int32_t* cache_len, int32_t n_streams, int32_t max_pages, int32_t n_pages, int32_t page_size,
+                     int32_t max_cache_len, const float* weights, int32_t weight_rows, int32_t budget, int32_t n_first,
+                     int32_t n_last, const int32_t* new_table, int32_t new_max_pages, int32_t* kept_out, int32_t* len_out,
+                     float* weights_out, int32_t weight_rows_out, void* workspace, size_t workspace_bytes, void* stream);
+size_t earn_cache_evict_workspace_bytes(const earn_attn_desc* desc, int32_t n_streams, int32_t max_cache_len, int32_t budget);
+
+/*
+ * The next token of every row of logits, drawn with uniform numbers that the caller gives (beside earn_beam_topk, for decoding
+ * without beams).  With T the row's temperature and l_max its largest logit, token i weighs w_i = exp((l_i - l_max) / T); the
+ * tokens stand in the order (logit descending, index ascending), and of them are kept
+ *   top-k   the first k                                       (k <= 0, or at least the number of tokens: all)
+ *   top-p   the shortest beginning that weighs at least p times what the first k weigh            (p >= 1: all)
+ *   min-p   those with w_i >= min_p                                                            (min_p <= 0: all; above 1 counts as 1)
+ * (each keeps a beginning of the order: the shortest one holds).  The token drawn is the lowest kept index t for which the
+ * kept w_0 + ... + w_t exceed u times the weight W of all kept.  T not above 0, or p not above 0: the first token of the order.
+ * NaN counts as -inf; -inf is never drawn or kept; with infinite logits those alone are kept, at equal weights; a row without
+ * any finite or infinite logit gives token -1, log-probability -inf, 0 kept.  u is cut to [0, 1).
+ * Weights are held as 64-bit integers, w_i 2^44 rounded: a token of less than 2^-45 of the best one's probability is never
+ * drawn, and no order of summation decides.
+ *   logits       [rows, vocab], dtype EARN_F32 or EARN_BF16, row r at logits + r * row_stride elements (any row_stride >= vocab)
+ *   uniform      [rows] fp32
+ *   temperature, top_p, min_p  [rows] fp32, top_k  [rows] int32; each may be NULL (1, all, all, all)
+ *   token_out    [rows] int32
+ *   logprob_out  [rows] fp32 or NULL: ln(w_t / W), 0 for the first token taken without drawing
+ *   n_kept_out   [rows] int32 or NULL: how many tokens were kept
+ *   workspace    at least earn_sample_workspace_bytes(rows, vocab) bytes, 256-byte aligned; may be NULL when that is 0
+ * All arrays in device memory.  Errors: NULL logits, uniform or token_out, non-positive size, row_stride < vocab -> INVALID_ARG;
+ * unknown dtype, vocab > 524288 -> UNSUPPORTED.  rows == 0 is a no-op.
+ */
+int earn_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
+                const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* token_out,
+                float* logprob_out, int32_t* n_kept_out, void* workspace, size_t workspace_bytes, void* stream);
+size_t earn_sample_workspace_bytes(int32_t rows, int32_t vocab);
 
 /*
  * Attention-score statistics of chosen query rows (paper Appendix, "Quantitative Measurements of Attention Score

@@ -272,3 +272,125 @@ def gamma_attn(n_layers: int, split_k: int, L: float, r: float, n_h: float, d_a:
 def causal_attn_flops(lengths, hq: int, d: int) -> float:
     ln = _i32(lengths)
     return float(lib().oracle_causal_attn_flops(_i(ln), len(ln), hq, d))
+
+
+# ---- caches in pages: plain loops over streams and heads, fp64 ----
+def paged_rows(pages, table_row, c: int, n: int):
+    """Rows 0 .. n - 1 of kv head c of a stream [n, d], and which of them have a page [n]."""
+    n_pages, _, size, d = pages.shape
+    rows, there = np.zeros((n, d)), np.zeros(n, dtype=bool)
+    for r in range(n):
+        page = int(table_row[r // size])
+        if 0 <= page < n_pages:
+            rows[r], there[r] = pages[page, c, r % size], True
+    return rows, there
+
+
+def paged_store(k, v, cu_seqlens, start, k_pages, v_pages, table) -> None:
+    """Rows of packed sequences to their pages (in place on k_pages / v_pages, any dtype)."""
+    n_pages, _, size, _ = k_pages.shape
+    for s in range(len(cu_seqlens) - 1):
+        for i in range(int(cu_seqlens[s + 1]) - int(cu_seqlens[s])):
+            r = i + (0 if start is None else int(start[s]))
+            if r // size >= table.shape[1]:
+                continue
+            page = int(table[s, r // size])
+            if 0 <= page < n_pages:
+                k_pages[page, :, r % size] = k[cu_seqlens[s] + i]
+                v_pages[page, :, r % size] = v[cu_seqlens[s] + i]
+
+
+def paged_decode(q, k_new, v_new, q_pos, k_pages, v_pages, table, cache_len, scale: float = 0.0, rope_base: float = 10000.0,
+                 q_to_kv=None, stored_key=None) -> dict:
+    """One decode step over pages.  stored_key [S, Hkv, d]: the new keys as the cache holds them (None: unrounded).
+    Returns dict(out [S, Hq, d], key [S, Hkv, d] (rotated, unrounded), probs: per stream [Hq, n + 1] or None for an idle one,
+    terms [S, Hq]: the largest sum over a row of the magnitudes that a score adds up, times scale)."""
+    q, k_new, v_new = _f64(q), _f64(k_new), _f64(v_new)
+    streams, hq, d = q.shape
+    hkv = k_new.shape[1]
+    group = hq // hkv
+    scale = scale if scale > 0 else 1.0 / np.sqrt(d)
+    pos = np.where(np.asarray(cache_len) < 0, 0, np.asarray(q_pos))
+    qr, kr = (rope(x, pos, rope_base) if rope_base > 0 else x for x in (q, k_new))
+    new = kr if stored_key is None else _f64(stored_key)
+    out, terms, probs = np.zeros_like(q), np.zeros((streams, hq)), []
+    for u in range(streams):
+        n = int(cache_len[u])
+        if n < 0:
+            probs.append(None)
+            continue
+        p_u = np.zeros((hq, n + 1))
+        for c in range(hkv):
+            keys, there = paged_rows(k_pages, table[u], c, n)
+            values, _ = paged_rows(v_pages, table[u], c, n)
+            keys, values = np.vstack([keys, new[u, c]]), np.vstack([values, v_new[u, c]])
+            there = np.append(there, True)
+            for a in range(hq):
+                if (q_to_kv[a] if q_to_kv is not None else a // group) != c:
+                    continue
+                s = np.where(there, (keys * qr[u, a]).sum(1) * scale, -np.inf)
+                e = np.exp(s - s.max())
+                p_u[a] = e / e.sum()
+                out[u, a] = p_u[a] @ values
+                terms[u, a] = (np.abs(keys[there]) * np.abs(qr[u, a])).sum(1).max() * scale
+        probs.append(p_u)
+    return {"out": out, "key": kr, "probs": probs, "terms": terms}
+
+
+def cache_evict(weights, cache_len, budget: int, n_first: int, n_last: int) -> list:
+    """kept[u][c]: the rows that stay, ascending (an idle stream: none)."""
+    kept = []
+    for u, n in enumerate(cache_len):
+        n = int(n)
+        if n <= budget:
+            kept.append([list(range(max(n, 0))) for _ in range(weights.shape[1])])
+            continue
+        per_head = []
+        for c in range(weights.shape[1]):
+            w = [float(x) for x in weights[u, c, :n]]
+            rest = sorted(range(n_first, n - n_last), key=lambda r: (w[r] != w[r], -w[r] if w[r] == w[r] else 0.0, r))
+            per_head.append(sorted(list(range(n_first)) + rest[:budget - n_first - n_last] + list(range(n - n_last, n))))
+        kept.append(per_head)
+    return kept
+
+
+def sample_token(logits, u: float, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0) -> dict:
+    """One row by the definition (a token of less than 2^-45 of the best one's weight weighs nothing): dict(token, logprob,
+    n_kept, margin), margin: how near to a border the choices came, in units of the best token's weight."""
+    l = np.asarray(logits, dtype=np.float64)
+    l = np.where(np.isnan(l), -np.inf, l)
+    order = np.argsort(-l, kind="stable")
+    order = order[l[order] > -np.inf]
+    if len(order) == 0:
+        return {"token": -1, "logprob": -np.inf, "n_kept": 0, "margin": 1.0}
+    if not temperature > 0 or not top_p > 0:
+        return {"token": int(order[0]), "logprob": 0.0, "n_kept": 1, "margin": 1.0}
+    best = l[order[0]]
+    if best == np.inf:
+        order = order[l[order] == np.inf]
+        w = np.ones(len(order))
+    else:
+        w = np.exp((l[order] - best) / temperature)
+    real, w = w, np.where(w < 2.0 ** -45, 0.0, w)
+    margin = 1.0
+    n = len(w) if top_k <= 0 else min(top_k, len(w))
+    if top_p < 1:
+        c = np.cumsum(w[:n])
+        at = c - top_p * c[-1]
+        margin = min(margin, float(np.abs(at).min()))
+        n = int(np.argmax(at >= 0)) + 1
+    if min_p > 0:
+        n = min(n, int((real >= min(min_p, 1.0)).sum()))
+    kept = np.sort(order[:n])
+    w_of = dict(zip(order.tolist(), w.tolist()))
+    wk = np.array([w_of[int(i)] for i in kept])
+    c = np.cumsum(wk) / wk.sum()
+    u = min(max(u, 0.0), 1.0 - 2.0 ** -24) if u == u else 0.0
+    at = int(np.argmax(c > u))
+    borders = c[:-1][c[:-1] > 0]
+    if u == 0:                  # the first token that weighs anything: near only to weighing nothing
+        weighs = real[: n][np.argsort(order[:n])][: at + 1]
+        margin = min(margin, float(np.abs(weighs * 2.0 ** 45 - 1).min()))
+    elif len(borders):
+        margin = min(margin, float(np.abs(borders - u).min() * wk.sum()))
+    return {"token": int(kept[at]), "logprob": float(np.log(wk[at] / wk.sum())), "n_kept": n, "margin": margin}

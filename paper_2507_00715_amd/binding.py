@@ -29,7 +29,9 @@ EXPORTS = ["earn_last_error", "earn_version", "earn_prefill_attn", "earn_prefill
            "earn_set_tuning", "earn_decode_attn_static", "earn_prefill_attn_layers", "earn_decode_attn_layers",
            "earn_decode_layers_workspace_bytes", "earn_decode_step_positions", "earn_attn_stats", "earn_beam_topk", "earn_beam_topk_workspace_bytes",
            "earn_beam_reorder", "earn_decode_attn_beams", "earn_qkv_rope_project", "earn_linear", "earn_linear_workspace_bytes", "earn_attn_backward",
-           "earn_attn_backward_workspace_bytes"]
+           "earn_attn_backward_workspace_bytes", "earn_cache_store",
+           "earn_decode_attn_paged", "earn_decode_paged_workspace_bytes", "earn_cache_evict", "earn_cache_evict_workspace_bytes",
+           "earn_sample", "earn_sample_workspace_bytes"]
 EARN_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -109,6 +111,22 @@ def lib():
         L.earn_prefill_register_rows_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, i32]
         L.earn_decode_workspace_bytes.restype = sz
         L.earn_decode_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, i32, i32]
+        L.earn_cache_store.restype = ctypes.c_int
+        L.earn_cache_store.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, i32, vp]
+        L.earn_decode_attn_paged.restype = ctypes.c_int
+        L.earn_decode_attn_paged.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp,
+                                             vp, i32, vp, vp, sz, vp]
+        L.earn_decode_paged_workspace_bytes.restype = sz
+        L.earn_decode_paged_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, i32]
+        L.earn_cache_evict.restype = ctypes.c_int
+        L.earn_cache_evict.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i32, i32, i32, i32, vp,
+                                       i32, vp, vp, vp, i32, vp, sz, vp]
+        L.earn_cache_evict_workspace_bytes.restype = sz
+        L.earn_cache_evict_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, i32]
+        L.earn_sample.restype = ctypes.c_int
+        L.earn_sample.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.earn_sample_workspace_bytes.restype = sz
+        L.earn_sample_workspace_bytes.argtypes = [i32, i32]
         L.earn_cache_entries.restype = ctypes.c_int64
         L.earn_cache_entries.argtypes = [i32, i32, ctypes.c_int64, i32, ctypes.c_int64]
         L.earn_set_validation.restype = ctypes.c_int
@@ -439,3 +457,112 @@ def earn_decode_attn_layers(desc: AttnDesc, q, k_new, v_new, q_pos, shared_k, sh
 
 def earn_cache_entries(n_layers: int, split_k: int, seq_len: int, n_registers: int, gen: int = 0) -> int:
     return int(lib().earn_cache_entries(n_layers, split_k, seq_len, n_registers, gen))
+
+
+def _ws(workspace, need: int, device):
+    """A workspace and its size: the caller's, or one for this call (loops pass a buffer of their own)."""
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace, (0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def _typed(dtype: torch.dtype, **tensors) -> None:
+    """The library is told no element types of index and weight arrays: they have to be what the header says."""
+    for name, t in tensors.items():
+        assert t is None or t.dtype == dtype, f"{name} must be {dtype}"
+
+
+def _pool(k_pages, v_pages, desc: AttnDesc):
+    """(n_pages, page_size) of [n_pages, Hkv, page_size, d] pools."""
+    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape, "k_pages, v_pages: [n_pages, Hkv, page_size, d]"
+    assert k_pages.shape[1] == desc.n_kv_heads and k_pages.shape[3] == desc.head_dim, "the pools have other heads than the description"
+    assert k_pages.element_size() == v_pages.element_size() == (4 if desc.dtype == EARN_F32 else 2), "the pools have another type than the description"
+    return k_pages.shape[0], k_pages.shape[2]
+
+
+def earn_cache_store(desc: AttnDesc, k, v, cu_seqlens, start, k_pages, v_pages, page_table) -> None:
+    """Rows of a prefill to their pages; cu_seqlens [batch + 1], start [batch] or None, page_table [batch, max_pages]."""
+    n_pages, page_size = _pool(k_pages, v_pages, desc)
+    _typed(torch.int32, cu_seqlens=cu_seqlens, start=start, page_table=page_table)
+    batch = page_table.shape[0]
+    assert cu_seqlens.numel() == batch + 1 and (start is None or start.numel() == batch) and k.shape == v.shape
+    assert tuple(k.shape[1:]) == (desc.n_kv_heads, desc.head_dim) and k.dtype == v.dtype == k_pages.dtype
+    _check(lib().earn_cache_store(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(start), batch, _rows(k),
+                                  _ptr(k_pages), _ptr(v_pages), _ptr(page_table), page_table.shape[1], n_pages, page_size,
+                                  _stream()))
+
+
+def earn_decode_paged_workspace_bytes(desc: AttnDesc, n_streams: int, max_cache_len: int, have_weights: bool) -> int:
+    return int(lib().earn_decode_paged_workspace_bytes(ctypes.byref(desc), n_streams, max_cache_len, int(bool(have_weights))))
+
+
+def bind_decode_attn_paged(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len: int,
+                           out, weights_in=None, weights_out=None, workspace=None) -> BoundCall:
+    """earn_decode_attn_paged with the same arguments, marshalled once (see BoundCall)."""
+    n_pages, page_size = _pool(k_pages, v_pages, desc)
+    n = page_table.shape[0]
+    _typed(torch.int32, q_pos=q_pos, page_table=page_table, cache_len=cache_len)
+    _typed(torch.float32, weights_in=weights_in, weights_out=weights_out)
+    _typed(k_pages.dtype, q=q, k_new=k_new, v_new=v_new, out=out)
+    assert q_pos.numel() == cache_len.numel() == n and q.shape == out.shape == (n, desc.n_q_heads, desc.head_dim)
+    assert k_new.shape == v_new.shape == (n, desc.n_kv_heads, desc.head_dim)
+    rows = 0
+    if weights_out is not None:
+        rows = weights_out.shape[-1]
+        assert tuple(weights_out.shape) == (n, desc.n_kv_heads, rows)
+        assert weights_in is None or weights_in.shape == weights_out.shape
+    workspace, ws_bytes = _ws(workspace, earn_decode_paged_workspace_bytes(desc, n, max_cache_len, weights_out is not None)
+                              if workspace is None else 0, q.device)
+    args = (ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_pos), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+            _ptr(cache_len), n, page_table.shape[1], n_pages, page_size, max_cache_len, _ptr(weights_in), _ptr(weights_out), rows,
+            _ptr(out), _ptr(workspace), ws_bytes)
+    return BoundCall(lib().earn_decode_attn_paged, args, (desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len,
+                                                          weights_in, weights_out, out, workspace))
+
+
+def earn_decode_attn_paged(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len: int,
+                           out, weights_in=None, weights_out=None, workspace=None) -> None:
+    bind_decode_attn_paged(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len, out, weights_in,
+                           weights_out, workspace)()
+
+
+def earn_cache_evict_workspace_bytes(desc: AttnDesc, n_streams: int, max_cache_len: int, budget: int) -> int:
+    return int(lib().earn_cache_evict_workspace_bytes(ctypes.byref(desc), n_streams, max_cache_len, budget))
+
+
+def earn_cache_evict(desc: AttnDesc, k_pages, v_pages, page_table, cache_len, max_cache_len: int, weights, budget: int,
+                     n_first: int, n_last: int, new_table, kept_out, len_out, weights_out=None, workspace=None) -> None:
+    n_pages, page_size = _pool(k_pages, v_pages, desc)
+    n, hkv = page_table.shape[0], desc.n_kv_heads
+    _typed(torch.int32, page_table=page_table, cache_len=cache_len, new_table=new_table, kept_out=kept_out, len_out=len_out)
+    _typed(torch.float32, weights=weights, weights_out=weights_out)
+    assert cache_len.numel() == len_out.numel() == n and new_table.shape[0] == n
+    assert tuple(weights.shape[:2]) == (n, hkv) and tuple(kept_out.shape) == (n, hkv, budget)
+    assert weights_out is None or tuple(weights_out.shape[:2]) == (n, hkv)
+    workspace, ws_bytes = _ws(workspace, earn_cache_evict_workspace_bytes(desc, n, max_cache_len, budget) if workspace is None else 0,
+                              k_pages.device)
+    _check(lib().earn_cache_evict(ctypes.byref(desc), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_len), n,
+                                  page_table.shape[1], n_pages, page_size, max_cache_len, _ptr(weights), weights.shape[2], budget,
+                                  n_first, n_last, _ptr(new_table), new_table.shape[1], _ptr(kept_out), _ptr(len_out),
+                                  _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2], _ptr(workspace), ws_bytes,
+                                  _stream()))
+
+
+def earn_sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(lib().earn_sample_workspace_bytes(rows, vocab))
+
+
+def earn_sample(logits, uniform, token_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob_out=None,
+                n_kept_out=None, workspace=None) -> None:
+    """logits [rows, vocab], fp32 or bf16, rows at any distance (a slice of wider rows is taken as it is)."""
+    code = {torch.float32: EARN_F32, torch.bfloat16: EARN_BF16}.get(logits.dtype, 99)
+    rows, vocab = logits.shape
+    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1), "the logits of a row must lie side by side"
+    _typed(torch.float32, uniform=uniform, temperature=temperature, top_p=top_p, min_p=min_p, logprob_out=logprob_out)
+    _typed(torch.int32, top_k=top_k, token_out=token_out, n_kept_out=n_kept_out)
+    for t in (uniform, token_out, temperature, top_k, top_p, min_p, logprob_out, n_kept_out):
+        assert t is None or t.numel() == rows, "one entry a row"
+    workspace, ws_bytes = _ws(workspace, earn_sample_workspace_bytes(rows, vocab) if workspace is None else 0, logits.device)
+    _check(lib().earn_sample(ctypes.c_void_p(logits.data_ptr()), code, logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                             _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(token_out),
+                             _ptr(logprob_out), _ptr(n_kept_out), _ptr(workspace), ws_bytes, _stream()))

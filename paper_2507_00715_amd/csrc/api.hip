@@ -82,6 +82,21 @@ size_t attn_backward_workspace_bytes(int hq, int total_tokens);
 int launch_attn_backward(const earn_attn_desc* desc, const void* q, const void* k, const void* v, const void* out,
                          const float* lse, const void* d_out, const int32_t* cu_seqlens, int batch, int total_tokens,
                          int max_seqlen, void* dq, void* dk, void* dv, void* workspace, hipStream_t stream);
+int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu, const int32_t* start, int batch,
+                       int total, void* k_pages, void* v_pages, const int32_t* table, int max_pages, int n_pages, int page_size,
+                       hipStream_t stream);
+size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights);
+int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new, const int32_t* q_pos,
+                        void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len, int n_streams, int max_pages,
+                        int n_pages, int page_size, int max_len, const float* w_in, float* w_out, int w_cap, void* out,
+                        void* workspace, hipStream_t stream);
+int launch_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len,
+                       int n_streams, int max_pages, int n_pages, int page_size, int max_len, const float* w_in, int w_cap, int budget,
+                       int first, int last, const int32_t* new_table, int new_pages, int32_t* kept, int32_t* len_out, float* w_out,
+                       int w_out_cap, hipStream_t stream);
+int launch_sample(const void* logits, int dtype, int64_t row_stride, int rows, int vocab, const float* temperature,
+                  const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* token,
+                  float* logprob, int32_t* n_kept, hipStream_t stream);
 int launch_rope_keys(const earn_attn_desc* desc, const void* k, void* k_rot, const int32_t* cu_seqlens,
                      const int32_t* positions, int batch, int total_tokens, hipStream_t stream);
 int launch_prefill_rows_f32(const earn_attn_desc* desc, const void* q_rows, const void* k_rot, const void* v,
@@ -190,6 +205,44 @@ static int validate_decode(const char* who, const int32_t* q_pos, const int32_t*
       if (++per_seq[s2s[u]] > 1024) { set_error("%s: sequence %d holds more than 1024 streams", who, s2s[u]); return EARN_ERR_INVALID_ARG; }
     }
   }
+  return EARN_OK;
+}
+
+// Tables and lengths of a call over pages: rows [0, rows[u]) of every stream lie in pages of the pool.
+static int validate_table(const char* who, const char* name, const std::vector<int32_t>& table, int streams, int max_pages, int n_pages,
+                          int page_size, const std::vector<long long>& rows) {
+  for (int u = 0; u < streams; ++u) {
+    if (rows[u] > (long long)max_pages * page_size) {
+      set_error("%s: stream %d has %lld rows, more than the %d pages of %s hold", who, u, rows[u], max_pages, name);
+      return EARN_ERR_INVALID_ARG;
+    }
+    for (long long i = 0; i * page_size < rows[u]; ++i) {
+      const int page = table[(size_t)u * max_pages + i];
+      if (page < 0 || page >= n_pages) {
+        set_error("%s: %s[%d][%lld] = %d outside [0, n_pages = %d)", who, name, u, i, page, n_pages);
+        return EARN_ERR_INVALID_ARG;
+      }
+    }
+  }
+  return EARN_OK;
+}
+// Pages [from[u], to[u]) of every stream are written: none of them is named twice, nor among the pages [0, from[u]) of a stream
+// or the pages that `taken` counts.
+static int validate_written(const char* who, const char* name, const std::vector<int32_t>& table, int streams, int max_pages,
+                            const std::vector<long long>& from, const std::vector<long long>& to, std::vector<int32_t>& taken) {
+  for (int u = 0; u < streams; ++u)
+    for (long long i = 0; i < to[u]; ++i) ++taken[table[(size_t)u * max_pages + i]];
+  for (int u = 0; u < streams; ++u)
+    for (long long i = from[u]; i < to[u]; ++i)
+      if (taken[table[(size_t)u * max_pages + i]] > 1) {
+        set_error("%s: page %d (%s[%d][%lld]) is written to and named elsewhere too", who, table[(size_t)u * max_pages + i], name, u, i);
+        return EARN_ERR_INVALID_ARG;
+      }
+  return EARN_OK;
+}
+static int validate_lengths(const char* who, const std::vector<int32_t>& len, int max_len) {
+  for (size_t u = 0; u < len.size(); ++u)
+    if (len[u] > max_len) { set_error("%s: cache_len[%zu] = %d, more than the bound %d passed by value", who, u, len[u], max_len); return EARN_ERR_INVALID_ARG; }
   return EARN_OK;
 }
 
@@ -640,6 +693,199 @@ int earn_attn_backward(const earn_attn_desc* desc, const void* q, const void* k,
   if (max_seqlen > total_tokens) max_seqlen = total_tokens;
   return launch_attn_backward(desc, q, k, v, out, lse, d_out, cu_seqlens, batch, total_tokens, max_seqlen, dq, dk, dv,
                               workspace, (hipStream_t)stream);
+}
+
+static int check_pages(const char* who, const void* k_pages, const void* v_pages, const int32_t* table, int32_t max_pages,
+                       int32_t n_pages, int32_t page_size) {
+  if (!k_pages || !v_pages || !table) { set_error("%s: k_pages, v_pages and page_table must not be NULL", who); return EARN_ERR_INVALID_ARG; }
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages) & 15) { set_error("%s: k_pages and v_pages must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
+  if (max_pages <= 0 || n_pages <= 0 || page_size <= 0) {
+    set_error("%s: max_pages (%d), n_pages (%d) and page_size (%d) must be positive", who, max_pages, n_pages, page_size);
+    return EARN_ERR_INVALID_ARG;
+  }
+  return EARN_OK;
+}
+static int check_workspace(const char* who, size_t need, const void* workspace, size_t bytes) {
+  if (need > bytes || (need > 0 && !workspace)) {
+    set_error("%s: workspace too small (%zu bytes given, %zu needed)", who, bytes, need);
+    return EARN_ERR_WORKSPACE_TOO_SMALL;
+  }
+  return EARN_OK;
+}
+
+int earn_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* start,
+                     int32_t batch, int32_t total_tokens, void* k_pages, void* v_pages, const int32_t* page_table,
+                     int32_t max_pages, int32_t n_pages, int32_t page_size, void* stream) {
+  const char* who = "earn_cache_store";
+  g_err[0] = 0;
+  int rc = check_desc(desc, who);
+  if (rc != EARN_OK) return rc;
+  if (batch <= 0 || total_tokens < 0) { set_error("%s: batch (%d) must be positive, total_tokens (%d) non-negative", who, batch, total_tokens); return EARN_ERR_INVALID_ARG; }
+  if ((rc = check_pages(who, k_pages, v_pages, page_table, max_pages, n_pages, page_size)) != EARN_OK) return rc;
+  if (!cu_seqlens) { set_error("%s: cu_seqlens is NULL", who); return EARN_ERR_INVALID_ARG; }
+  if (total_tokens == 0) return EARN_OK;
+  if (!k || !v) { set_error("%s: k and v must not be NULL", who); return EARN_ERR_INVALID_ARG; }
+  if (((uintptr_t)k | (uintptr_t)v) & 15) { set_error("%s: k and v must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
+  if (g_validate.load(std::memory_order_relaxed)) {
+    std::vector<int32_t> cu, st((size_t)batch, 0), table;
+    if ((rc = fetch_i32(cu_seqlens, (size_t)batch + 1, cu, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = validate_cu(who, "cu_seqlens", cu, batch, total_tokens, 0x7fffffff)) != EARN_OK) return rc;
+    if (start && (rc = fetch_i32(start, (size_t)batch, st, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = fetch_i32(page_table, (size_t)batch * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    std::vector<long long> rows((size_t)batch), from((size_t)batch), to((size_t)batch);
+    for (int s = 0; s < batch; ++s) {
+      if (st[s] < 0) { set_error("%s: start[%d] = %d is negative", who, s, st[s]); return EARN_ERR_INVALID_ARG; }
+      const int n = cu[s + 1] - cu[s];
+      rows[s] = n > 0 ? (long long)st[s] + n : 0;
+      to[s] = (rows[s] + page_size - 1) / page_size;
+      from[s] = n > 0 ? st[s] / page_size : to[s];
+    }
+    if ((rc = validate_table(who, "page_table", table, batch, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+    std::vector<int32_t> taken((size_t)n_pages, 0);
+    if ((rc = validate_written(who, "page_table", table, batch, max_pages, from, to, taken)) != EARN_OK) return rc;
+  }
+  return launch_cache_store(desc, k, v, cu_seqlens, start, batch, total_tokens, k_pages, v_pages, page_table, max_pages, n_pages,
+                            page_size, (hipStream_t)stream);
+}
+
+// what the kernels over pages take beyond the description's own checks; sizes of the grid
+static int check_paged_desc(const earn_attn_desc* d, int32_t n_streams, const char* who) {
+  const int rc = check_desc(d, who);
+  if (rc != EARN_OK) return rc;
+  if (d->n_q_heads / d->n_kv_heads > 128) { set_error("%s: more than 128 query heads per kv head", who); return EARN_ERR_UNSUPPORTED; }
+  if (n_streams > 65535 || d->n_q_heads > 65535) { set_error("%s: more than 65535 streams or heads", who); return EARN_ERR_UNSUPPORTED; }
+  return EARN_OK;
+}
+
+size_t earn_decode_paged_workspace_bytes(const earn_attn_desc* desc, int32_t n_streams, int32_t max_cache_len,
+                                         int32_t have_weights) {
+  if (check_paged_desc(desc, n_streams, "earn_decode_paged_workspace_bytes") != EARN_OK || n_streams <= 0 || max_cache_len < 0 ||
+      max_cache_len > EARN_MAX_CACHE_LEN)
+    return 0;
+  return decode_paged_workspace_bytes(desc, n_streams, max_cache_len, have_weights != 0);
+}
+
+int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new,
+                           const int32_t* q_pos, void* k_pages, void* v_pages, const int32_t* page_table,
+                           const int32_t* cache_len, int32_t n_streams, int32_t max_pages, int32_t n_pages,
+                           int32_t page_size, int32_t max_cache_len, const float* weights_in, float* weights_out,
+                           int32_t weight_rows, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "earn_decode_attn_paged";
+  g_err[0] = 0;
+  int rc = check_paged_desc(desc, n_streams, who);
+  if (rc != EARN_OK) return rc;
+  if (n_streams <= 0 || max_cache_len < 0 || max_cache_len > EARN_MAX_CACHE_LEN) {
+    set_error("%s: n_streams (%d) must be positive, max_cache_len (%d) in [0, %d]", who, n_streams, max_cache_len, EARN_MAX_CACHE_LEN);
+    return EARN_ERR_INVALID_ARG;
+  }
+  if ((rc = check_pages(who, k_pages, v_pages, page_table, max_pages, n_pages, page_size)) != EARN_OK) return rc;
+  if (!q || !k_new || !v_new || !q_pos || !cache_len || !out) { set_error("%s: a required pointer is NULL", who); return EARN_ERR_INVALID_ARG; }
+  if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) { set_error("%s: q, k_new, v_new and out must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
+  if (weights_in && !weights_out) { set_error("%s: weights_in without weights_out", who); return EARN_ERR_INVALID_ARG; }
+  if (weights_out && weight_rows <= 0) { set_error("%s: weight_rows (%d) must be positive", who, weight_rows); return EARN_ERR_INVALID_ARG; }
+  const size_t need = decode_paged_workspace_bytes(desc, n_streams, max_cache_len, weights_out != nullptr);
+  if ((rc = check_workspace(who, need, workspace, workspace_bytes)) != EARN_OK) return rc;
+  if (g_validate.load(std::memory_order_relaxed)) {
+    std::vector<int32_t> qp, len, table;
+    if ((rc = fetch_i32(q_pos, (size_t)n_streams, qp, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
+    std::vector<long long> rows((size_t)n_streams), from((size_t)n_streams), to((size_t)n_streams);
+    for (int u = 0; u < n_streams; ++u) {
+      if (len[u] < 0) qp[u] = 0;                   // an idle stream's position is not read
+      rows[u] = len[u] < 0 ? 0 : (long long)len[u] + 1;
+      to[u] = (rows[u] + page_size - 1) / page_size;
+      from[u] = rows[u] > 0 ? to[u] - 1 : 0;
+    }
+    if ((rc = validate_positions(who, "q_pos", qp)) != EARN_OK) return rc;
+    if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+    std::vector<int32_t> taken((size_t)n_pages, 0);
+    if ((rc = validate_written(who, "page_table", table, n_streams, max_pages, from, to, taken)) != EARN_OK) return rc;
+  }
+  return launch_decode_paged(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages,
+                             page_size, max_cache_len, weights_in, weights_out, weight_rows, out, workspace, (hipStream_t)stream);
+}
+
+size_t earn_cache_evict_workspace_bytes(const earn_attn_desc* desc, int32_t n_streams, int32_t max_cache_len, int32_t budget) {
+  (void)desc; (void)n_streams; (void)max_cache_len; (void)budget;
+  return 0;
+}
+
+int earn_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, const int32_t* page_table,
+                     const int32_t* cache_len, int32_t n_streams, int32_t max_pages, int32_t n_pages, int32_t page_size,
+                     int32_t max_cache_len, const float* weights, int32_t weight_rows, int32_t budget, int32_t n_first,
+                     int32_t n_last, const int32_t* new_table, int32_t new_max_pages, int32_t* kept_out, int32_t* len_out,
+                     float* weights_out, int32_t weight_rows_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "earn_cache_evict";
+  g_err[0] = 0;
+  int rc = check_paged_desc(desc, n_streams, who);
+  if (rc != EARN_OK) return rc;
+  if (n_streams <= 0 || max_cache_len < 0 || max_cache_len > EARN_MAX_CACHE_LEN || budget <= 0 || weight_rows <= 0) {
+    set_error("%s: n_streams (%d), budget (%d) and weight_rows (%d) must be positive, max_cache_len (%d) in [0, %d]", who, n_streams, budget, weight_rows, max_cache_len, EARN_MAX_CACHE_LEN);
+    return EARN_ERR_INVALID_ARG;
+  }
+  if (n_first < 0 || n_last < 0 || (long long)n_first + n_last > budget) {
+    set_error("%s: n_first (%d) and n_last (%d) must be non-negative and together at most budget (%d)", who, n_first, n_last, budget);
+    return EARN_ERR_INVALID_ARG;
+  }
+  if ((rc = check_pages(who, k_pages, v_pages, page_table, max_pages, n_pages, page_size)) != EARN_OK) return rc;
+  if (!cache_len || !weights || !new_table || !kept_out || !len_out) { set_error("%s: a required pointer is NULL", who); return EARN_ERR_INVALID_ARG; }
+  if (max_cache_len > weight_rows) { set_error("%s: max_cache_len (%d) exceeds weight_rows (%d)", who, max_cache_len, weight_rows); return EARN_ERR_INVALID_ARG; }
+  if (new_max_pages <= 0 || (long long)new_max_pages * page_size < budget) {
+    set_error("%s: %d new pages of %d rows do not hold budget = %d rows", who, new_max_pages, page_size, budget);
+    return EARN_ERR_INVALID_ARG;
+  }
+  if (weights_out == weights) { set_error("%s: weights_out must not be weights", who); return EARN_ERR_INVALID_ARG; }
+  if (weights_out && weight_rows_out < budget) { set_error("%s: weight_rows_out (%d) is less than budget (%d)", who, weight_rows_out, budget); return EARN_ERR_INVALID_ARG; }
+  if ((rc = check_workspace(who, earn_cache_evict_workspace_bytes(desc, n_streams, max_cache_len, budget), workspace, workspace_bytes)) != EARN_OK) return rc;
+  if (g_validate.load(std::memory_order_relaxed)) {
+    std::vector<int32_t> len, table, fresh;
+    if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
+    if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    if ((rc = fetch_i32(new_table, (size_t)n_streams * new_max_pages, fresh, (hipStream_t)stream, who)) != EARN_OK) return rc;
+    std::vector<long long> rows((size_t)n_streams), kept((size_t)n_streams), zero((size_t)n_streams, 0), to((size_t)n_streams);
+    for (int u = 0; u < n_streams; ++u) {
+      rows[u] = len[u] < 0 ? 0 : len[u];
+      kept[u] = rows[u] < budget ? rows[u] : budget;
+      to[u] = (kept[u] + page_size - 1) / page_size;
+    }
+    if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+    if ((rc = validate_table(who, "new_table", fresh, n_streams, new_max_pages, n_pages, page_size, kept)) != EARN_OK) return rc;
+    std::vector<int32_t> taken((size_t)n_pages, 0);
+    for (int u = 0; u < n_streams; ++u)
+      for (long long i = 0; i * page_size < rows[u]; ++i) taken[table[(size_t)u * max_pages + i]] = 1;
+    if ((rc = validate_written(who, "new_table", fresh, n_streams, new_max_pages, zero, to, taken)) != EARN_OK) return rc;
+  }
+  return launch_cache_evict(desc, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages, page_size, max_cache_len,
+                            weights, weight_rows, budget, n_first, n_last, new_table, new_max_pages, kept_out, len_out, weights_out,
+                            weight_rows_out, (hipStream_t)stream);
+}
+
+size_t earn_sample_workspace_bytes(int32_t rows, int32_t vocab) {
+  (void)rows; (void)vocab;
+  return 0;
+}
+
+int earn_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
+                const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* token_out,
+                float* logprob_out, int32_t* n_kept_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "earn_sample";
+  g_err[0] = 0;
+  if (dtype != EARN_F32 && dtype != EARN_BF16) { set_error("%s: unknown dtype %d", who, dtype); return EARN_ERR_UNSUPPORTED; }
+  if (rows < 0 || vocab <= 0 || row_stride < vocab) {
+    set_error("%s: rows (%d) must be non-negative, vocab (%d) positive, row_stride (%lld) at least vocab", who, rows, vocab, (long long)row_stride);
+    return EARN_ERR_INVALID_ARG;
+  }
+  if (vocab > 524288) { set_error("%s: vocab (%d) beyond 524288", who, vocab); return EARN_ERR_UNSUPPORTED; }
+  if (rows == 0) return EARN_OK;
+  if (!logits || !uniform || !token_out) { set_error("%s: logits, uniform and token_out must not be NULL", who); return EARN_ERR_INVALID_ARG; }
+  if ((uintptr_t)logits & (dtype == EARN_F32 ? 3 : 1)) { set_error("%s: logits are not aligned to their type", who); return EARN_ERR_INVALID_ARG; }
+  const int rc = check_workspace(who, earn_sample_workspace_bytes(rows, vocab), workspace, workspace_bytes);
+  if (rc != EARN_OK) return rc;
+  return launch_sample(logits, dtype, row_stride, rows, vocab, temperature, top_k, top_p, min_p, uniform, token_out, logprob_out,
+                       n_kept_out, (hipStream_t)stream);
 }
 
 int64_t earn_cache_entries(int32_t n_layers, int32_t split_k, int64_t seq_len, int32_t n_registers, int64_t gen) {

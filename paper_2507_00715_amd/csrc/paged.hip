@@ -1,0 +1,582 @@
+// Caches in pages: a stream's rows lie in pages of `page_size` rows, [n_pages, Hkv, page_size, d], that a table names in the
+// order of its rows.  A (page, kv head) is contiguous, so that the rows a workgroup reads for one kv head are.
+//   paged_store_kernel   rows of a prefill to their pages
+//   paged_decode_kernel  one new token per stream: append, then attention over the pages (paper Section 2.2, Eq. 4)
+//   paged_join_kernel    joins the splits of long caches; running sums of the weights every row received
+//   evict_select_kernel, evict_move_kernel  the rows of largest sums, to fresh pages
+// No value of a table or a length reaches past the pools: a page number outside them names no page (its rows are not
+// attended, stored to it is nothing).
+#include <type_traits>
+
+#include "common.h"
+#include "decode_pieces.h"
+
+namespace earn {
+
+// Pools and tables, as all kernels here take them.
+struct Pages {
+  void* k; void* v;            // [n_pages, hkv, page_size, d]
+  const int32_t* table;        // [streams, max_pages]
+  int max_pages, n_pages, page_size, hkv;
+  FastDiv by_page;             // row -> page of the stream
+};
+// The stream's page that holds row r, -1: none.  (r < max_pages * page_size)
+__device__ __forceinline__ int page_of_row(const Pages& pg, int u, int r, int& in_page) {
+  const int at = (int)pg.by_page.div((unsigned)r);
+  in_page = r - at * pg.page_size;
+  const int page = pg.table[(long long)u * pg.max_pages + at];
+  return (unsigned)page < (unsigned)pg.n_pages ? page : -1;
+}
+// Element offset of row `in_page` of kv head c in a pool.
+template <int D>
+__device__ __forceinline__ long long row_offset(const Pages& pg, int page, int c, int in_page) {
+  return (((long long)page * pg.hkv + c) * pg.page_size + in_page) * D;
+}
+__device__ __forceinline__ int capacity_of(const Pages& pg) {   // rows that a table's pages hold
+  return (int)min((long long)pg.max_pages * pg.page_size, 0x7fffff00ll);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// store: 16 bytes of a K and a V row per thread
+// ------------------------------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_store_kernel(const T* __restrict__ k, const T* __restrict__ v, Pages pg,
+                                                          const int32_t* __restrict__ cu, const int32_t* __restrict__ start,
+                                                          int batch, int total) {
+  constexpr int UPR = D * (int)sizeof(T) / 16;   // 16-byte units of a row
+  const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long row = t / UPR;                 // (token, kv head)
+  const int unit = (int)(t % UPR);
+  const int token = (int)(row / pg.hkv), c = (int)(row % pg.hkv);
+  if (token >= total) return;
+  const int s = find_seq(cu, batch, token);
+  int b0, n;
+  clamped_bounds(cu, s, total, total, b0, n);
+  if (token < b0 || token >= b0 + n) return;     // behind the last sequence
+  const long long r = (long long)(token - b0) + (start ? start[s] : 0);
+  if (r < 0 || r >= capacity_of(pg)) return;
+  int in_page;
+  const int page = page_of_row(pg, s, (int)r, in_page);
+  if (page < 0) return;
+  const long long to = row_offset<D>(pg, page, c, in_page) * (long long)sizeof(T) / 16 + unit;
+  ((u32x4*)pg.k)[to] = ((const u32x4*)k)[t];
+  ((u32x4*)pg.v)[to] = ((const u32x4*)v)[t];
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// decode
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / kWave;
+constexpr int kPagedMaxChunk = 2048;   // rows of a split: its page numbers lie in LDS
+
+struct PagedParams {
+  Pages pg;
+  const void* q; const void* k_new; const void* v_new; const int32_t* q_pos; const int32_t* cache_len;
+  const float* w_in; float* w_out;       // [streams, hkv, w_cap]
+  void* out;
+  float* part_o; float* part_ml;         // [streams, hq, n_splits, d], [.., 2]
+  float* scores;                         // [streams, hq, score_stride], base-2 exponents
+  int n_streams, hq, hkv, w_cap, max_len, n_splits, chunk, score_stride;
+  float scale_log2;
+  RopeTable rope;
+  HeadMap heads;
+};
+
+// rows of stream u before this step, -1: an idle stream
+__device__ __forceinline__ int length_of(const int32_t* cache_len, int u, int max_len, const Pages& pg) {
+  const int n = cache_len[u];
+  return n < 0 ? -1 : min(min(n, max_len), capacity_of(pg));
+}
+
+// One head's 8 elements of a workgroup's result: a split's state, or the output.
+template <typename T, int D>
+__device__ __forceinline__ void finish_group(const PagedParams& p, long long first_head, int slot_head, int z, int e, float m, float l, float* x) {
+  if (p.part_o) {
+    const long long slot = (first_head + slot_head) * p.n_splits + z;
+    *(f32x4*)(p.part_o + slot * D + e) = f32x4{x[0], x[1], x[2], x[3]};
+    *(f32x4*)(p.part_o + slot * D + e + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    if (e == 0) *(f32x2*)(p.part_ml + slot * 2) = f32x2{m, l};
+  } else {
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= inv;
+    Row8<T>::store((T*)p.out + (first_head + head_of_slot(p.heads, slot_head)) * D + e, x);
+  }
+}
+
+template <typename T, int D, int GQ>
+__global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams p) {
+  constexpr int LPK = D / 8, KPW = kWave / LPK;      // lanes per row, rows per wave instruction
+  constexpr int NP = GQ >= 8 ? 2 : Row8<T>::kRowsInFlight;
+  constexpr int STEP = kPagedWaves * KPW;
+  __shared__ int pages[kPagedMaxChunk + 2];
+  __shared__ float merge[kPagedWaves][GQ][LPK][10];
+  const int gq = p.hq / p.hkv, parts = (gq + GQ - 1) / GQ;
+  const int z = blockIdx.x, c = blockIdx.y / parts, a0 = (int)(blockIdx.y % parts) * GQ, u = blockIdx.z;
+  const int na = min(gq - a0, GQ);                   // query heads of this workgroup
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, sub = lane % LPK, kk = lane / LPK;
+  const int n = length_of(p.cache_len, u, p.max_len, p.pg);
+  if (n < 0) {                                       // idle: zeros
+    if (z == 0)
+      for (int i = tid; i < na * LPK; i += kPagedThreads) {
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Row8<T>::store((T*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + i / LPK)) * D + i % LPK * 8, zero);
+      }
+    return;
+  }
+  const int j_begin = z * p.chunk, j_end = min(n + 1, j_begin + p.chunk);
+  if (j_begin >= j_end) return;
+  const bool has_new = j_end == n + 1;
+  const int page0 = (int)p.pg.by_page.div((unsigned)j_begin);
+  {
+    const int last = (int)p.pg.by_page.div((unsigned)max(j_begin, min(j_end, n) - 1));
+    for (int i = page0 + tid; i <= min(last, p.pg.max_pages - 1); i += kPagedThreads) {
+      const int page = p.pg.table[(long long)u * p.pg.max_pages + i];
+      pages[i - page0] = (unsigned)page < (unsigned)p.pg.n_pages ? page : -1;
+    }
+  }
+  // queries and the new key, rotated
+  float cs[8], sn[8];
+  const float pos = (float)p.q_pos[u];
+  const int e0 = (sub * 8) % (D / 2);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.f; sn[i] = 0.f;
+    if (p.rope.enabled) sincos_turns_precise(rope_turns(pos, p.rope.hi[e0 + i], p.rope.lo[e0 + i]), &sn[i], &cs[i]);
+  }
+  const bool upper = sub * 8 >= D / 2;
+  auto rotate = [&](float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float other = __shfl_xor(x[i], LPK / 2, kWave);
+      x[i] = upper ? __builtin_fmaf(x[i], cs[i], other * sn[i]) : __builtin_fmaf(x[i], cs[i], -(other * sn[i]));
+    }
+  };
+  float qv[GQ][8], kn[8], vn[8];
+#pragma unroll
+  for (int a = 0; a < GQ; ++a) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qv[a][i] = 0.f;
+    if (a < na) {
+      Row8<T>::load((const T*)p.q + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + a)) * D + sub * 8, qv[a]);
+      rotate(qv[a]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qv[a][i] *= p.scale_log2;
+    }
+  }
+  Row8<T>::load((const T*)p.k_new + ((long long)u * p.hkv + c) * D + sub * 8, kn);
+  Row8<T>::load((const T*)p.v_new + ((long long)u * p.hkv + c) * D + sub * 8, vn);
+  rotate(kn);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) kn[i] = Row8<T>::round(kn[i]);
+  __syncthreads();
+  const T* K = (const T*)p.pg.k + sub * 8;
+  const T* V = (const T*)p.pg.v + sub * 8;
+  if (has_new && a0 == 0 && wave == 0 && kk == 0 && n < capacity_of(p.pg)) {   // cache append
+    int in_page;
+    const int page = page_of_row(p.pg, u, n, in_page);
+    if (page >= 0) {
+      const long long to = row_offset<D>(p.pg, page, c, in_page) + sub * 8;
+      Row8<T>::store((T*)p.pg.k + to, kn);
+      Row8<T>::store((T*)p.pg.v + to, vn);
+    }
+  }
+  float mx[GQ], ls[GQ], o[GQ][8];
+#pragma unroll
+  for (int a = 0; a < GQ; ++a) {
+    mx[a] = -INFINITY; ls[a] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[a][i] = 0.f;
+  }
+  for (int jb = j_begin + wave * KPW; jb < j_end; jb += NP * STEP) {
+    typename Row8<T>::Raw kr[NP], vr[NP];
+    bool there[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int j = jb + i * STEP + kk;
+      kr[i] = typename Row8<T>::Raw{}; vr[i] = typename Row8<T>::Raw{};
+      there[i] = j == n && j < j_end;
+      if (j < n && j < j_end) {
+        const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
+        if (page >= 0) {
+          const long long from = row_offset<D>(p.pg, page, c, j - at * p.pg.page_size);
+          kr[i] = Row8<T>::load_raw(K + from);
+          vr[i] = Row8<T>::load_raw(V + from);
+          there[i] = true;
+        }
+      }
+    }
+    float sc[NP][GQ];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int j = jb + i * STEP + kk;
+      float kx[8];
+      Row8<T>::unpack(kr[i], kx);
+      if (j == n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) kx[e] = kn[e];
+      }
+#pragma unroll
+      for (int a = 0; a < GQ; ++a) {
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d = __builtin_fmaf(qv[a][e], kx[e], d);
+        d = group_sum<LPK>(d);
+        sc[i][a] = there[i] ? d : -INFINITY;
+        if (p.scores && sub == 0 && a < na && j < j_end)
+          p.scores[((long long)u * p.hq + c * gq + a0 + a) * p.score_stride + j] = sc[i][a];
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < GQ; ++a) {
+      float mn = mx[a];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) mn = fmaxf(mn, sc[i][a]);
+      const float corr = mx[a] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx[a] - mn);
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        sc[i][a] = sc[i][a] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc[i][a] - mn);
+        sum += sc[i][a];
+      }
+      ls[a] = ls[a] * corr + sum;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[a][e] *= corr;
+      mx[a] = mn;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      float vx[8];
+      Row8<T>::unpack(vr[i], vx);
+      if (jb + i * STEP + kk == n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vx[e] = vn[e];
+      }
+#pragma unroll
+      for (int a = 0; a < GQ; ++a)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[a][e] = __builtin_fmaf(sc[i][a], vx[e], o[a][e]);
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < GQ; ++a) {
+#pragma unroll
+    for (int off = LPK; off < kWave; off <<= 1) {
+      const float m2 = __shfl_xor(mx[a], off, kWave), l2 = __shfl_xor(ls[a], off, kWave);
+      float o2[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o2[i] = __shfl_xor(o[a][i], off, kWave);
+      merge_state<8>(mx[a], ls[a], o[a], m2, l2, o2);
+    }
+  }
+  if (kk == 0) {
+#pragma unroll
+    for (int a = 0; a < GQ; ++a) {
+      merge[wave][a][sub][0] = mx[a];
+      merge[wave][a][sub][1] = ls[a];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) merge[wave][a][sub][2 + i] = o[a][i];
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < na * LPK; i += kPagedThreads) {
+    const int a = i / LPK, sb = i % LPK;
+    float m = merge[0][a][sb][0], l = merge[0][a][sb][1], x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = merge[0][a][sb][2 + e];
+#pragma unroll
+    for (int w = 1; w < kPagedWaves; ++w) merge_state<8>(m, l, x, merge[w][a][sb][0], merge[w][a][sb][1], &merge[w][a][sb][2]);
+    finish_group<T, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, sb * 8, m, l, x);
+  }
+}
+
+// Joins the splits' states: block x = 0 of a (kv head, stream) the outputs, the others 1024 rows' weights each.
+constexpr int kJoinRows = 1024;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
+  constexpr int LPK = D / 8;
+  const int c = blockIdx.y, u = blockIdx.z, gq = p.hq / p.hkv, tid = threadIdx.x;
+  const int n = length_of(p.cache_len, u, p.max_len, p.pg);
+  if (n < 0) return;
+  const int used = (n + p.chunk) / p.chunk;    // splits that have rows: n + 1 rows
+  const long long head0 = (long long)u * p.hq + c * gq;
+  if (blockIdx.x == 0) {
+    for (int i = tid; i < gq * LPK; i += 256) {
+      const int a = i / LPK, sb = i % LPK;
+      float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int z = 0; z < used; ++z) {
+        const long long slot = (head0 + a) * p.n_splits + z;
+        float x2[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x2[e] = p.part_o[slot * D + sb * 8 + e];
+        merge_state<8>(m, l, x, p.part_ml[slot * 2], p.part_ml[slot * 2 + 1], x2);
+      }
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= inv;
+      Row8<T>::store((T*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a)) * D + sb * 8, x);
+    }
+    return;
+  }
+  const int j0 = (int)(blockIdx.x - 1) * kJoinRows, j1 = min(min(n + 1, j0 + kJoinRows), p.w_cap);
+  if (j0 >= j1) return;
+  __shared__ float ref[128], inv[128];
+  for (int a = tid; a < min(gq, 128); a += 256) {
+    float m = -INFINITY, l = 0.f;
+    for (int z = 0; z < used; ++z) m = fmaxf(m, p.part_ml[((head0 + a) * p.n_splits + z) * 2]);
+    for (int z = 0; z < used; ++z) {
+      const float mz = p.part_ml[((head0 + a) * p.n_splits + z) * 2], lz = p.part_ml[((head0 + a) * p.n_splits + z) * 2 + 1];
+      l += mz == -INFINITY ? lz : lz * __builtin_amdgcn_exp2f(mz - m);
+    }
+    ref[a] = m;
+    inv[a] = 1.f / l;
+  }
+  __syncthreads();
+  const long long to = ((long long)u * p.hkv + c) * p.w_cap;
+  for (int j = j0 + tid; j < j1; j += 256) {
+    float w = 0.f;
+    for (int a = 0; a < gq; ++a) {
+      const float s = p.scores[(head0 + a) * p.score_stride + j];
+      w += s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - ref[a]) * inv[a];
+    }
+    p.w_out[to + j] = (j < n && p.w_in ? p.w_in[to + j] : 0.f) + w;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// evict
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
+
+struct EvictParams {
+  Pages pg;
+  const int32_t* cache_len; const float* w_in; float* w_out; const int32_t* new_table;
+  int32_t* kept; int32_t* len_out;
+  int n_streams, max_len, w_cap, w_out_cap, budget, first, last, new_pages;
+};
+
+// a weight as an integer of the same order: NaN below everything, zeros of either sign equal
+__device__ __forceinline__ unsigned weight_key(float w) {
+  if (w != w) return 0u;
+  const unsigned b = __float_as_uint(w == 0.f ? 0.f : w);
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+// One workgroup per (kv head, stream): the key of the last row that is kept by weight, bit by bit from the top, then the kept
+// rows in their order.  A wave has a run of rows of its own.
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
+  __shared__ int counts[kSelectWaves], counts2[kSelectWaves];
+  const int c = blockIdx.x, u = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int n = length_of(p.cache_len, u, min(p.max_len, p.w_cap), p.pg);
+  const long long pair = (long long)u * p.pg.hkv + c;
+  const float* w = p.w_in + pair * p.w_cap;
+  int32_t* kept = p.kept + pair * p.budget;
+  float* w_out = p.w_out ? p.w_out + pair * p.w_out_cap : nullptr;
+  const int m = min(n, p.budget);
+  for (int i = max(m, 0) + tid; i < p.budget; i += kSelectThreads) kept[i] = -1;
+  if (n < 0) return;
+  if (n <= p.budget) {
+    for (int i = tid; i < n; i += kSelectThreads) {
+      kept[i] = i;
+      if (w_out) w_out[i] = w[i];
+    }
+    return;
+  }
+  const int lo = p.first, hi = n - p.last, need = p.budget - p.first - p.last;   // rows [lo, hi) compete for `need` places
+  const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + kWave - 1) / kWave * kWave;
+  const int begin = lo + wave * per, end = min(hi, begin + per);
+  // (a wave's count of rows whose key satisfies cmp; summed over the workgroup)
+  auto count_all = [&](auto cmp) {
+    int mine = 0;
+    for (int j = begin; j < end; j += kWave) mine += __popcll(__ballot(j + lane < end && cmp(weight_key(w[min(j + lane, end - 1)]))));
+    __syncthreads();
+    if (lane == 0) counts[wave] = mine;
+    __syncthreads();
+    int all = 0;
+    for (int i = 0; i < kSelectWaves; ++i) all += counts[i];
+    return all;
+  };
+  // the largest key t that at least `need` rows reach
+  unsigned t = 0;
+  if (need > 0)
+    for (int bit = 31; bit >= 0; --bit) {
+      const unsigned with = t | 1u << bit;
+      if (count_all([with](unsigned k) { return k >= with; }) >= need) t = with;
+    }
+  const int equal_kept = need - (need > 0 ? count_all([t](unsigned k) { return k > t; }) : 0);
+  // where each wave's equal rows and kept rows begin
+  int above = 0, equal = 0;
+  for (int j = begin; j < end && need > 0; j += kWave) {
+    const unsigned k = weight_key(w[min(j + lane, end - 1)]);
+    above += __popcll(__ballot(j + lane < end && k > t));
+    equal += __popcll(__ballot(j + lane < end && k == t));
+  }
+  __syncthreads();
+  if (lane == 0) { counts[wave] = above; counts2[wave] = equal; }
+  __syncthreads();
+  int at = p.first, eq = 0;
+  for (int i = 0; i < wave; ++i) { at += counts[i]; eq += counts2[i]; }
+  at += min(eq, equal_kept);
+  for (int i = tid; i < p.first; i += kSelectThreads) {
+    kept[i] = i;
+    if (w_out) w_out[i] = w[i];
+  }
+  for (int j = begin; j < end && need > 0; j += kWave) {
+    const float x = w[min(j + lane, end - 1)];
+    const unsigned k = weight_key(x);
+    const unsigned long long before = (1ull << lane) - 1, is_equal = __ballot(j + lane < end && k == t);
+    const bool keep = j + lane < end && (k > t || (k == t && eq + __popcll(is_equal & before) < equal_kept));
+    const unsigned long long mask = __ballot(keep);
+    if (keep) {
+      const int to = at + __popcll(mask & before);
+      kept[to] = j + lane;
+      if (w_out) w_out[to] = x;
+    }
+    at += __popcll(mask);
+    eq += __popcll(is_equal);
+  }
+  for (int i = tid; i < p.last; i += kSelectThreads) {
+    kept[p.budget - p.last + i] = hi + i;
+    if (w_out) w_out[p.budget - p.last + i] = w[hi + i];
+  }
+}
+
+// 16 bytes of a K and a V row per thread
+template <typename T, int D>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
+  constexpr int UPR = D * (int)sizeof(T) / 16;
+  const int i = (int)(blockIdx.x * (256 / UPR) + threadIdx.x / UPR), unit = threadIdx.x % UPR, c = blockIdx.y, u = blockIdx.z;
+  if (blockIdx.x == 0 && c == 0 && threadIdx.x == 0 && p.len_out) {
+    const int n = length_of(p.cache_len, u, min(p.max_len, p.w_cap), p.pg);
+    p.len_out[u] = min(n, p.budget);
+  }
+  if (i >= p.budget) return;
+  const int r = p.kept[((long long)u * p.pg.hkv + c) * p.budget + i];
+  if (r < 0) return;
+  int in_old;
+  const int old = page_of_row(p.pg, u, r, in_old);
+  const int at = (int)p.pg.by_page.div((unsigned)i), page = p.new_table[(long long)u * p.new_pages + at];
+  if ((unsigned)page >= (unsigned)p.pg.n_pages) return;
+  const long long to = row_offset<D>(p.pg, page, c, i - at * p.pg.page_size) * (long long)sizeof(T) / 16 + unit;
+  u32x4 k = {0u, 0u, 0u, 0u}, v = k;             // a row without a page: zeros
+  if (old >= 0) {
+    const long long from = row_offset<D>(p.pg, old, c, in_old) * (long long)sizeof(T) / 16 + unit;
+    k = ((const u32x4*)p.pg.k)[from];
+    v = ((const u32x4*)p.pg.v)[from];
+  }
+  ((u32x4*)p.pg.k)[to] = k;
+  ((u32x4*)p.pg.v)[to] = v;
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------------------------------------
+static Pages make_pages(void* k, void* v, const int32_t* table, int max_pages, int n_pages, int page_size, int hkv) {
+  return Pages{k, v, table, max_pages, n_pages, page_size, hkv, FastDiv::of((unsigned)page_size)};
+}
+static int launched() {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return EARN_OK;
+  set_error("launch failed: %s", hipGetErrorString(e));
+  return EARN_ERR_HIP;
+}
+// f(T{}, std::integral_constant<int, D>{}) for the description's type and head size
+template <typename F>
+static void for_type(const earn_attn_desc* desc, F f) {
+  const bool f32 = desc->dtype == EARN_F32;
+  if (desc->head_dim == 64) { if (f32) f(float{}, std::integral_constant<int, 64>{}); else f(__bf16{}, std::integral_constant<int, 64>{}); }
+  else { if (f32) f(float{}, std::integral_constant<int, 128>{}); else f(__bf16{}, std::integral_constant<int, 128>{}); }
+}
+
+int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu, const int32_t* start, int batch,
+                       int total, void* k_pages, void* v_pages, const int32_t* table, int max_pages, int n_pages, int page_size,
+                       hipStream_t stream) {
+  const Pages pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
+  const long long units = (long long)total * desc->n_kv_heads * (desc->head_dim * (desc->dtype == EARN_F32 ? 4 : 2) / 16);
+  for_type(desc, [&](auto t, auto d) {
+    typedef decltype(t) T;
+    hipLaunchKernelGGL((paged_store_kernel<T, decltype(d)::value>), dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream,
+                       (const T*)k, (const T*)v, pg, cu, start, batch, total);
+  });
+  return launched();
+}
+
+struct PagedPlan { int n_splits, chunk, score_stride; size_t part_o, part_ml, scores; };
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
+  PagedPlan pl{};
+  const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
+  long long splits = (1024 + pairs - 1) / pairs;
+  if (splits > (rows + 255) / 256) splits = (rows + 255) / 256;
+  if (splits < (rows + kPagedMaxChunk - 1) / kPagedMaxChunk) splits = (rows + kPagedMaxChunk - 1) / kPagedMaxChunk;
+  pl.chunk = (int)(((rows + splits - 1) / splits + 63) / 64 * 64);
+  pl.n_splits = (int)((rows + pl.chunk - 1) / pl.chunk);
+  pl.score_stride = (int)((rows + 31) / 32 * 32);   // whole blocks of rows
+  const size_t heads = (size_t)n_streams * desc->n_q_heads;
+  if (pl.n_splits > 1 || weights) {
+    pl.part_o = up256(heads * pl.n_splits * desc->head_dim * 4);
+    pl.part_ml = up256(heads * pl.n_splits * 8);
+  }
+  if (weights) pl.scores = up256(heads * pl.score_stride * 4);
+  return pl;
+}
+size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
+  const PagedPlan pl = plan_paged(desc, n_streams, max_len, weights);
+  return pl.part_o + pl.part_ml + pl.scores;
+}
+
+int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new, const int32_t* q_pos,
+                        void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len, int n_streams, int max_pages,
+                        int n_pages, int page_size, int max_len, const float* w_in, float* w_out, int w_cap, void* out,
+                        void* workspace, hipStream_t stream) {
+  const PagedPlan pl = plan_paged(desc, n_streams, max_len, w_out != nullptr);
+  PagedParams p;
+  p.pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
+  p.q = q; p.k_new = k_new; p.v_new = v_new; p.q_pos = q_pos; p.cache_len = cache_len;
+  p.w_in = w_in; p.w_out = w_out; p.out = out; p.w_cap = w_cap;
+  p.part_o = pl.part_o ? (float*)workspace : nullptr;
+  p.part_ml = (float*)((char*)workspace + pl.part_o);
+  p.scores = pl.scores ? (float*)((char*)workspace + pl.part_o + pl.part_ml) : nullptr;
+  p.n_streams = n_streams; p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.max_len = max_len;
+  p.n_splits = pl.n_splits; p.chunk = pl.chunk; p.score_stride = pl.score_stride;
+  const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.f / sqrtf((float)desc->head_dim);
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.rope = make_rope_table(desc->rope_base, desc->head_dim);
+  const int rc = make_head_map(desc, &p.heads, "earn_decode_attn_paged");
+  if (rc != EARN_OK) return rc;
+  const int gq = p.hq / p.hkv, g = gq > 4 ? 8 : gq > 2 ? 4 : gq, parts = (gq + g - 1) / g;
+  const dim3 grid(pl.n_splits, p.hkv * parts, n_streams);
+  for_type(desc, [&](auto t, auto d) {
+    typedef decltype(t) T;
+    constexpr int D = decltype(d)::value;
+    if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (g == 2) hipLaunchKernelGGL((paged_decode_kernel<T, D, 2>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (g == 4) hipLaunchKernelGGL((paged_decode_kernel<T, D, 4>), grid, dim3(kPagedThreads), 0, stream, p);
+    else hipLaunchKernelGGL((paged_decode_kernel<T, D, 8>), grid, dim3(kPagedThreads), 0, stream, p);
+    if (p.part_o) {
+      const int row_blocks = w_out ? (int)(((long long)max_len + kJoinRows) / kJoinRows) : 0;
+      hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(1 + row_blocks, p.hkv, n_streams), dim3(256), 0, stream, p);
+    }
+  });
+  return launched();
+}
+
+int launch_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len,
+                       int n_streams, int max_pages, int n_pages, int page_size, int max_len, const float* w_in, int w_cap, int budget,
+                       int first, int last, const int32_t* new_table, int new_pages, int32_t* kept, int32_t* len_out, float* w_out,
+                       int w_out_cap, hipStream_t stream) {
+  EvictParams p;
+  p.pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
+  p.cache_len = cache_len; p.w_in = w_in; p.w_out = w_out; p.new_table = new_table; p.kept = kept; p.len_out = len_out;
+  p.n_streams = n_streams; p.max_len = max_len; p.w_cap = w_cap; p.w_out_cap = w_out_cap;
+  p.budget = budget; p.first = first; p.last = last; p.new_pages = new_pages;
+  hipLaunchKernelGGL(evict_select_kernel, dim3(desc->n_kv_heads, n_streams), dim3(kSelectThreads), 0, stream, p);
+  for_type(desc, [&](auto t, auto d) {
+    typedef decltype(t) T;
+    constexpr int D = decltype(d)::value, rows = 256 / (D * (int)sizeof(T) / 16);
+    hipLaunchKernelGGL((evict_move_kernel<T, D>), dim3((budget + rows - 1) / rows, desc->n_kv_heads, n_streams), dim3(256), 0, stream, p);
+  });
+  return launched();
+}
+
+}  // namespace earn
