@@ -290,6 +290,209 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
   }
 }
 
+// bf16: the same on the matrix cores.  Per block of 32 rows a wave computes
+//   S^T = K Q^T (16 keys x up to 16 query heads; the K fragments are plain 16-byte loads of rows, straight into registers)
+//   O^T += V^T P^T (V through a swizzled LDS tile of the wave's own; the layout of two S^T tiles is this product's operand)
+// with queries and weights as sums of three bf16 operands each, 24 significant bits, as in the short decode kernels.  While
+// a block is worked on, the next one's rows are on their way: its keys are asked for when this block's scores are done, its values
+// when this block's are in LDS.
+template <int D, int QR>
+__global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(PagedParams p) {
+  constexpr int KS = D / 32, DB = D / 16, UPR = D / 8, BLK = 32, NV = BLK * UPR / kWave;
+  union Tile { __bf16 v[BLK * D]; float o[QR][D + 4]; };
+  __shared__ Tile tile[kPagedWaves];
+  __shared__ f32x2 ml[kPagedWaves][QR];
+  __shared__ __align__(16) __bf16 rot[3][QR + 1][D + 8];   // queries in three terms; row QR of the first: the new key as stored
+  __shared__ int pages[kPagedMaxChunk + 2];
+  const int gq = p.hq / p.hkv, parts = (gq + QR - 1) / QR;
+  const int z = blockIdx.x, c = blockIdx.y / parts, a0 = (int)(blockIdx.y % parts) * QR, u = blockIdx.z;
+  const int na = min(gq - a0, QR);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int r16 = lane & 15, quad = lane >> 4;
+  const int n = length_of(p.cache_len, u, p.max_len, p.pg);
+  const int j_begin = z * p.chunk, j_end = min(n + 1, j_begin + p.chunk);
+  if (n < 0) {                                       // idle: zeros
+    if (z == 0)
+      for (int i = tid; i < na * UPR; i += kPagedThreads) {
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Row8<__bf16>::store((__bf16*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + i / UPR)) * D + i % UPR * 8, zero);
+      }
+    return;
+  }
+  if (j_begin >= j_end) return;
+  const int page0 = (int)p.pg.by_page.div((unsigned)j_begin);
+  {
+    const int last = min((int)p.pg.by_page.div((unsigned)max(j_begin, min(j_end, n) - 1)), p.pg.max_pages - 1);
+    for (int i = page0 + tid; i <= last; i += kPagedThreads) {
+      const int page = p.pg.table[(long long)u * p.pg.max_pages + i];
+      pages[i - page0] = (unsigned)page < (unsigned)p.pg.n_pages ? page : -1;
+    }
+  }
+  const __bf16* new_k = (const __bf16*)p.k_new + ((long long)u * p.hkv + c) * D;
+  const __bf16* new_v = (const __bf16*)p.v_new + ((long long)u * p.hkv + c) * D;
+  // queries and the new key: 4 rotary pairs of a row per item
+  {
+    const float pos = (float)p.q_pos[u];
+    for (int item = tid; item < (na + 1) * (D / 8); item += kPagedThreads) {
+      const int row = item / (D / 8), e = item % (D / 8) * 4;
+      const bool key = row == na;
+      const __bf16* src = (key ? new_k : (const __bf16*)p.q + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + row)) * D) + e;
+      const u32x2 lo = *(const u32x2*)src, hi = *(const u32x2*)(src + D / 2);
+      const float scale = key ? 1.f : p.scale_log2;
+      float y[2][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float sn = 0.f, cs = 1.f;
+        if (p.rope.enabled) sincos_turns_precise(rope_turns(pos, p.rope.hi[e + j], p.rope.lo[e + j]), &sn, &cs);
+        const float a = j & 1 ? bf16_hi(lo[j / 2]) : bf16_lo(lo[j / 2]), b = j & 1 ? bf16_hi(hi[j / 2]) : bf16_lo(hi[j / 2]);
+        y[0][j] = __builtin_fmaf(a, cs, -(b * sn)) * scale;
+        y[1][j] = __builtin_fmaf(b, cs, a * sn) * scale;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        unsigned w0[3], w1[3];
+        split_pair(y[h][0], y[h][1], w0);
+        split_pair(y[h][2], y[h][3], w1);
+        if (key) *(u32x2*)&rot[0][QR][e + h * (D / 2)] = u32x2{w0[0], w1[0]};   // the first term: rounded as stored
+        else {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) *(u32x2*)&rot[i][row][e + h * (D / 2)] = u32x2{w0[i], w1[i]};
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (j_end == n + 1 && a0 == 0 && n < capacity_of(p.pg)) {   // cache append
+    int in_page;
+    const int page = page_of_row(p.pg, u, n, in_page);
+    if (page >= 0 && tid < 2 * UPR) {
+      const long long to = row_offset<D>(p.pg, page, c, in_page) + tid % UPR * 8;
+      if (tid < UPR) *(u32x4*)((__bf16*)p.pg.k + to) = *(const u32x4*)&rot[0][QR][tid * 8];
+      else *(u32x4*)((__bf16*)p.pg.v + to) = *(const u32x4*)(new_v + tid % UPR * 8);
+    }
+  }
+  const int n_blocks = (j_end - j_begin + BLK - 1) / BLK;
+  // element offset of row j (j_begin <= j < n) in a pool, -1: no page
+  auto row_at = [&](int j) {
+    const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
+    return page < 0 ? -1ll : row_offset<D>(p.pg, page, c, j - at * p.pg.page_size);
+  };
+  bf16x8 kf[2][KS];
+  u32x4 vr[NV];
+  unsigned there = 0;                                 // bit i: row i of the block has a key
+  auto load_keys = [&](int blk) {
+    const int j0 = j_begin + blk * BLK;
+    there = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int j = j0 + 16 * t + r16;
+      const __bf16* row = nullptr;
+      if (j < min(n, j_end)) {
+        const long long at = row_at(j);
+        if (at >= 0) row = (const __bf16*)p.pg.k + at;
+      }
+      there |= ((unsigned)__ballot(row != nullptr || (j == n && j < j_end)) & 0xffffu) << (16 * t);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        kf[t][ks] = bf16x8{};
+        if (row) kf[t][ks] = *(const bf16x8*)(row + 32 * ks + 8 * quad);
+      }
+    }
+  };
+  auto load_values = [&](int blk) {
+    const int j0 = j_begin + blk * BLK;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int unit = lane + kWave * i, j = j0 + unit / UPR;
+      vr[i] = u32x4{0u, 0u, 0u, 0u};
+      if (j < min(n, j_end)) {
+        const long long at = row_at(j);
+        if (at >= 0) vr[i] = *(const u32x4*)((const __bf16*)p.pg.v + at + unit % UPR * 8);
+      } else if (j == n && j < j_end) vr[i] = *(const u32x4*)(new_v + unit % UPR * 8);
+    }
+  };
+  f32x4 o[DB];
+  float mrow, lrow;
+  __bf16* smv = tile[wave].v;
+  const int q_row = min(r16, na - 1);                 // columns beyond the group repeat its last query
+  float* scores = p.scores ? p.scores + ((long long)u * p.hq + c * gq + a0 + q_row) * p.score_stride : nullptr;
+  auto walk = [&](auto careful_c) {
+    constexpr bool CAREFUL = decltype(careful_c)::value;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    mrow = -INFINITY;
+    lrow = 0.f;
+    if (wave < n_blocks) { load_keys(wave); load_values(wave); }
+    for (int blk = wave; blk < n_blocks; blk += kPagedWaves) {
+      const int j0 = j_begin + blk * BLK;
+      const unsigned mask = there;
+      if (blk == n_blocks - 1 && j_end == n + 1) {     // the new token's key
+        const int j = n - j0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const bf16x8 w = *(const bf16x8*)&rot[0][QR][32 * ks + 8 * quad];
+          if (j == r16) kf[0][ks] = w;
+          if (j == 16 + r16) kf[1][ks] = w;
+        }
+      }
+      f32x4 sc[2];
+      short_scores<D, QR + 1, CAREFUL>(kf, rot, q_row, quad, sc);
+      const bool more = blk + kPagedWaves < n_blocks;
+      if (more) load_keys(blk + kPagedWaves);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int unit = lane + kWave * i, row = unit / UPR;
+        *(u32x4*)(smv + row * D + (((unit % UPR) ^ short_v_swz<D>(row)) << 3)) = vr[i];
+      }
+      if (more) load_values(blk + kPagedWaves);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(mask >> (16 * t + 4 * quad + i) & 1)) sc[t][i] = -INFINITY;
+      if (scores && r16 < na) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) *(f32x4*)(scores + j0 + 16 * t + 4 * quad) = sc[t];
+      }
+      u32x4 pw[3];
+      const float alpha = short_softmax(sc, mrow, lrow, pw);
+      asm volatile("" ::: "memory");
+      short_weigh<D, CAREFUL>(smv, pw, alpha, lane, o);
+      asm volatile("" ::: "memory");
+    }
+  };
+  walk(std::false_type{});
+  float probe = lrow;                                 // NaN where anything is, or where infinities of both signs meet
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) probe += o[db][i];
+  if (__any(probe != probe)) walk(std::true_type{});
+  lrow += __shfl_xor(lrow, 16, kWave);
+  lrow += __shfl_xor(lrow, 32, kWave);
+  if (r16 < na) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *(f32x4*)&tile[wave].o[r16][16 * db + 4 * quad] = o[db];
+    if (quad == 0) ml[wave][r16] = f32x2{mrow, lrow};
+  }
+  __syncthreads();
+  for (int i = tid; i < na * UPR; i += kPagedThreads) {
+    const int a = i / UPR, e = (i % UPR) * 8;
+    float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) m = fmaxf(m, ml[w][a][0]);
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) {
+      if (w >= n_blocks) continue;                    // a wave without rows: its tile holds nothing
+      const float f = ml[w][a][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][a][0] - m);
+      l += f * ml[w][a][1];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(f, tile[w].o[a][e + j], x[j]);
+    }
+    finish_group<__bf16, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, e, m, l, x);
+  }
+}
+
 // Joins the splits' states: block x = 0 of a (kv head, stream) the outputs, the others 1024 rows' weights each.
 constexpr int kJoinRows = 1024;
 template <typename T, int D>
@@ -544,16 +747,24 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   p.rope = make_rope_table(desc->rope_base, desc->head_dim);
   const int rc = make_head_map(desc, &p.heads, "earn_decode_attn_paged");
   if (rc != EARN_OK) return rc;
-  const int gq = p.hq / p.hkv, g = gq > 4 ? 8 : gq > 2 ? 4 : gq, parts = (gq + g - 1) / g;
+  const bool mfma = desc->dtype == EARN_BF16;
+  const int gq = p.hq / p.hkv, g = mfma ? (gq > 8 ? 16 : 8) : gq > 4 ? 8 : gq > 2 ? 4 : gq, parts = (gq + g - 1) / g;
   const dim3 grid(pl.n_splits, p.hkv * parts, n_streams);
   for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
-    if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
+    if (mfma && g == 8) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (mfma) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if constexpr (sizeof(T) == 2) return;
+    else if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
     else if (g == 2) hipLaunchKernelGGL((paged_decode_kernel<T, D, 2>), grid, dim3(kPagedThreads), 0, stream, p);
     else if (g == 4) hipLaunchKernelGGL((paged_decode_kernel<T, D, 4>), grid, dim3(kPagedThreads), 0, stream, p);
     else hipLaunchKernelGGL((paged_decode_kernel<T, D, 8>), grid, dim3(kPagedThreads), 0, stream, p);
-    if (p.part_o) {
+  });
+  if (p.part_o) for_type(desc, [&](auto t, auto d) {
+    typedef decltype(t) T;
+    constexpr int D = decltype(d)::value;
+    {
       const int row_blocks = w_out ? (int)(((long long)max_len + kJoinRows) / kJoinRows) : 0;
       hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(1 + row_blocks, p.hkv, n_streams), dim3(256), 0, stream, p);
     }
