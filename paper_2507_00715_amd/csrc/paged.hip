@@ -88,6 +88,45 @@ __device__ __forceinline__ int length_of(const int32_t* cache_len, int u, int ma
   return n < 0 ? -1 : min(min(n, max_len), capacity_of(pg));
 }
 
+// The sums of rows [j0, j1) of a (stream, kv head), by the whole workgroup: old sums and the first head's scores are asked for
+// before `states` gives the heads' (reference, 1 / sum) in LDS, and waits for all threads.
+constexpr int kWeightRows = 4 * kPagedThreads;   // of one round
+template <typename States>
+__device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, int n, int j0, int j1, const f32x2* state, States states) {
+  const int gq = p.hq / p.hkv, tid = threadIdx.x;
+  const float* scores = p.scores + ((long long)u * p.hq + c * gq) * p.score_stride;
+  const long long to = ((long long)u * p.hkv + c) * p.w_cap;
+  bool first = true;
+  for (int jb = j0; jb < j1; jb += kWeightRows) {
+    float w[4], old[4], s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = jb + i * kPagedThreads + tid;
+      w[i] = 0.f;
+      old[i] = j < j1 && j < n && p.w_in ? p.w_in[to + j] : 0.f;
+      s[i] = j < j1 ? scores[j] : -INFINITY;
+    }
+    if (first) { states(); first = false; }
+    for (int a = 0; a < gq; ++a) {
+      if (a > 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = jb + i * kPagedThreads + tid;
+          s[i] = j < j1 ? scores[(long long)a * p.score_stride + j] : -INFINITY;
+        }
+      }
+      const f32x2 st = state[a];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] += s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[i] - st[0]) * st[1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = jb + i * kPagedThreads + tid;
+      if (j < j1) p.w_out[to + j] = old[i] + w[i];
+    }
+  }
+}
+
 // One head's 8 elements of a workgroup's result: a split's state, or the output.
 template <typename T, int D>
 __device__ __forceinline__ void finish_group(const PagedParams& p, long long first_head, int slot_head, int z, int e, float m, float l, float* x) {
@@ -111,8 +150,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
   constexpr int STEP = kPagedWaves * KPW;
   __shared__ int pages[kPagedMaxChunk + 2];
   __shared__ float merge[kPagedWaves][GQ][LPK][10];
+  __shared__ f32x2 states[GQ];
   const int gq = p.hq / p.hkv, parts = (gq + GQ - 1) / GQ;
-  const int z = blockIdx.x, c = blockIdx.y / parts, a0 = (int)(blockIdx.y % parts) * GQ, u = blockIdx.z;
+  const int z = blockIdx.z, c = blockIdx.x / parts, u = blockIdx.y, a0 = (int)(blockIdx.x % parts) * GQ;
   const int na = min(gq - a0, GQ);                   // query heads of this workgroup
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, sub = lane % LPK, kk = lane / LPK;
   const int n = length_of(p.cache_len, u, p.max_len, p.pg);
@@ -287,25 +327,31 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
 #pragma unroll
     for (int w = 1; w < kPagedWaves; ++w) merge_state<8>(m, l, x, merge[w][a][sb][0], merge[w][a][sb][1], &merge[w][a][sb][2]);
     finish_group<T, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, sb * 8, m, l, x);
+    if (sb == 0) states[a] = f32x2{m, 1.f / l};
   }
+  if (p.scores && !p.part_o) add_weights(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
 }
 
 // bf16: the same on the matrix cores.  Per block of 32 rows a wave computes
-//   S^T = K Q^T (16 keys x up to 16 query heads; the K fragments are plain 16-byte loads of rows, straight into registers)
-//   O^T += V^T P^T (V through a swizzled LDS tile of the wave's own; the layout of two S^T tiles is this product's operand)
-// with queries and weights as sums of three bf16 operands each, 24 significant bits, as in the short decode kernels.  While
-// a block is worked on, the next one's rows are on their way: its keys are asked for when this block's scores are done, its values
-// when this block's are in LDS.
-template <int D, int QR>
-__global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(PagedParams p) {
+//   S^T = K Q^T     (16 keys x up to 16 query heads)
+//   O^T += V^T P^T  (the layout of two S^T tiles is this product's operand)
+// with queries and weights as sums of three bf16 operands each, 24 significant bits, as in the short decode kernels.  Keys, then
+// values pass through one swizzled LDS tile of the wave's own: they leave memory whole lines at a time, as they lie there (key
+// fragments straight from memory touch half lines, which loads that leave nothing in the caches then fetch twice).  While a
+// block is worked on, the next one's rows are on their way: each half is asked for as soon as this block's is in LDS.
+// 16 consecutive rows have a chunk at different places: a fragment's reads meet no bank twice
+template <int D>
+__device__ __forceinline__ int key_swz(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+template <int D, int QR, bool STREAMED>
+__global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_mfma_kernel(PagedParams p) {
   constexpr int KS = D / 32, DB = D / 16, UPR = D / 8, BLK = 32, NV = BLK * UPR / kWave;
   union Tile { __bf16 v[BLK * D]; float o[QR][D + 4]; };
   __shared__ Tile tile[kPagedWaves];
-  __shared__ f32x2 ml[kPagedWaves][QR];
+  __shared__ f32x2 ml[kPagedWaves][QR], states[QR];
   __shared__ __align__(16) __bf16 rot[3][QR + 1][D + 8];   // queries in three terms; row QR of the first: the new key as stored
   __shared__ int pages[kPagedMaxChunk + 2];
   const int gq = p.hq / p.hkv, parts = (gq + QR - 1) / QR;
-  const int z = blockIdx.x, c = blockIdx.y / parts, a0 = (int)(blockIdx.y % parts) * QR, u = blockIdx.z;
+  const int z = blockIdx.z, c = blockIdx.x / parts, u = blockIdx.y, a0 = (int)(blockIdx.x % parts) * QR;
   const int na = min(gq - a0, QR);
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r16 = lane & 15, quad = lane >> 4;
@@ -322,9 +368,9 @@ __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(Pag
   if (j_begin >= j_end) return;
   const int page0 = (int)p.pg.by_page.div((unsigned)j_begin);
   {
-    const int last = min((int)p.pg.by_page.div((unsigned)max(j_begin, min(j_end, n) - 1)), p.pg.max_pages - 1);
-    for (int i = page0 + tid; i <= last; i += kPagedThreads) {
-      const int page = p.pg.table[(long long)u * p.pg.max_pages + i];
+    const int last = (int)p.pg.by_page.div((unsigned)max(j_begin, min(j_end, n) - 1));
+    for (int i = page0 + tid; i <= last; i += kPagedThreads) {   // (a table that is full has no page for row n)
+      const int page = i < p.pg.max_pages ? p.pg.table[(long long)u * p.pg.max_pages + i] : -1;
       pages[i - page0] = (unsigned)page < (unsigned)p.pg.n_pages ? page : -1;
     }
   }
@@ -372,48 +418,54 @@ __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(Pag
     }
   }
   const int n_blocks = (j_end - j_begin + BLK - 1) / BLK;
-  // element offset of row j (j_begin <= j < n) in a pool, -1: no page
-  auto row_at = [&](int j) {
-    const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
-    return page < 0 ? -1ll : row_offset<D>(p.pg, page, c, j - at * p.pg.page_size);
-  };
-  bf16x8 kf[2][KS];
-  u32x4 vr[NV];
-  unsigned there = 0;                                 // bit i: row i of the block has a key
-  auto load_keys = [&](int blk) {
+  // A block as it lies in memory: unit lane + 64 i of its rows, 16 bytes each.  Every unit is loaded, those of rows that are not
+  // there from some row that is in the pool.  Returns which rows are there.
+  // Whole blocks over pages of a multiple of 16 rows: 16 rows lie in one page, one behind the other, and a wave looks their pages
+  // up once (one row at a time, a block took 590 vector instructions, now 330).
+  constexpr int RPI = kWave / UPR;                    // rows of 64 units
+  const bool by_sixteen = p.pg.page_size % 16 == 0;
+  auto load_block = [&](u32x4 (&x)[NV], const __bf16* pool, int blk) {
     const int j0 = j_begin + blk * BLK;
-    there = 0;
+    unsigned have = 0;                                // bit i: row i of the block has a place in the pool
+    if (by_sixteen && j0 + BLK <= min(n, j_end)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int j = j0 + 16 * t + r16;
-      const __bf16* row = nullptr;
-      if (j < min(n, j_end)) {
-        const long long at = row_at(j);
-        if (at >= 0) row = (const __bf16*)p.pg.k + at;
-      }
-      there |= ((unsigned)__ballot(row != nullptr || (j == n && j < j_end)) & 0xffffu) << (16 * t);
+      for (int t = 0; t < 2; ++t) {
+        const int j = j0 + 16 * t, at = (int)p.pg.by_page.div((unsigned)j), page = __builtin_amdgcn_readfirstlane(pages[at - page0]);
+        const u32x4* rows = (const u32x4*)(pool + row_offset<D>(p.pg, max(page, 0), c, j - at * p.pg.page_size));
+        have |= page >= 0 ? 0xffffu << (16 * t) : 0u;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        kf[t][ks] = bf16x8{};
-        if (row) kf[t][ks] = *(const bf16x8*)(row + 32 * ks + 8 * quad);
+        for (int i = 0; i < NV / 2; ++i) x[t * (NV / 2) + i] = STREAMED ? __builtin_nontemporal_load(rows + lane + kWave * i) : rows[lane + kWave * i];
       }
+      return have;
     }
-  };
-  auto load_values = [&](int blk) {
-    const int j0 = j_begin + blk * BLK;
+    int own = lane;                                   // (opaque: what follows from it is not worth registers over the loop)
+    asm volatile("" : "+v"(own));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int unit = lane + kWave * i, j = j0 + unit / UPR;
-      vr[i] = u32x4{0u, 0u, 0u, 0u};
-      if (j < min(n, j_end)) {
-        const long long at = row_at(j);
-        if (at >= 0) vr[i] = *(const u32x4*)((const __bf16*)p.pg.v + at + unit % UPR * 8);
-      } else if (j == n && j < j_end) vr[i] = *(const u32x4*)(new_v + unit % UPR * 8);
+      const int unit = own + kWave * i, j = min(j0 + unit / UPR, max(min(n, j_end) - 1, j_begin));
+      const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
+      x[i] = *(const u32x4*)(pool + row_offset<D>(p.pg, max(page, 0), c, j - at * p.pg.page_size) + unit % UPR * 8);
+      const unsigned long long who = __ballot(page >= 0 && j0 + unit / UPR < min(n, j_end));
+#pragma unroll
+      for (int r = 0; r < RPI; ++r) have |= (unsigned)(who >> (r * UPR) & 1) << (i * RPI + r);
+      asm volatile("" ::: "memory");                  // one row's address at a time: together they do not fit the registers
     }
+    return have;
   };
+  const u32x4 newest = *(const u32x4*)(new_v + r16 % UPR * 8);
+  u32x4 kr[NV], vr[NV];
+  unsigned there = 0;
   f32x4 o[DB];
   float mrow, lrow;
   __bf16* smv = tile[wave].v;
+  // Byte addresses in the tile.  Unit lane + 64 i is chunk lane % UPR of row lane / UPR + RPI i, and lies at that chunk ^ swizzle(row):
+  // the lane's own part of it, ^ what the row's RPI i adds.
+  int key_write = lane / UPR * (2 * D) + ((lane % UPR ^ key_swz<D>(lane / UPR)) << 4), key_read = r16 * (2 * D) + ((quad ^ key_swz<D>(r16)) << 4);
+  int value_write = lane / UPR * (2 * D) + ((lane % UPR ^ short_v_swz<D>(lane / UPR)) << 4);
+  // of the transposing reads of 16 elements by 8 keys: keys 4 quad + (0..3), and 16 rows on
+  int value_read = (4 * quad + (r16 >> 2)) * (2 * D) + (((r16 & 3) >> 1 ^ short_v_swz<D>(4 * quad + (r16 >> 2))) << 4) + 8 * (r16 & 1);
+  auto key_step = [](int i) { return key_swz<D>(RPI * i) << 4; };
+  auto value_step = [](int i) { return short_v_swz<D>(RPI * i) << 4; };
   const int q_row = min(r16, na - 1);                 // columns beyond the group repeat its last query
   float* scores = p.scores ? p.scores + ((long long)u * p.hq + c * gq + a0 + q_row) * p.score_stride : nullptr;
   auto walk = [&](auto careful_c) {
@@ -422,34 +474,66 @@ __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(Pag
     for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     mrow = -INFINITY;
     lrow = 0.f;
-    if (wave < n_blocks) { load_keys(wave); load_values(wave); }
+    if (wave < n_blocks) {
+      there = load_block(kr, (const __bf16*)p.pg.k, wave);
+      load_block(vr, (const __bf16*)p.pg.v, wave);
+    }
     for (int blk = wave; blk < n_blocks; blk += kPagedWaves) {
       const int j0 = j_begin + blk * BLK;
-      const unsigned mask = there;
-      if (blk == n_blocks - 1 && j_end == n + 1) {     // the new token's key
-        const int j = n - j0;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const bf16x8 w = *(const bf16x8*)&rot[0][QR][32 * ks + 8 * quad];
-          if (j == r16) kf[0][ks] = w;
-          if (j == 16 + r16) kf[1][ks] = w;
-        }
-      }
-      f32x4 sc[2];
-      short_scores<D, QR + 1, CAREFUL>(kf, rot, q_row, quad, sc);
+      const unsigned stored = there;
       const bool more = blk + kPagedWaves < n_blocks;
-      if (more) load_keys(blk + kPagedWaves);
+      const int j_new = blk == n_blocks - 1 && j_end == n + 1 ? n - j0 : BLK;   // the new token's row of the block
+      const unsigned mask = j_new < BLK ? stored | 1u << j_new : stored;
+      // (opaque: eight addresses a register each, kept over the loop, would not fit)
+      asm volatile("" : "+v"(key_write), "+v"(key_read), "+v"(value_write), "+v"(value_read));
+      // the wave's LDS operations complete in order: only the compiler has to keep theirs
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int unit = lane + kWave * i, row = unit / UPR;
-        *(u32x4*)(smv + row * D + (((unit % UPR) ^ short_v_swz<D>(row)) << 3)) = vr[i];
+        *(u32x4*)((char*)smv + (key_write ^ key_step(i)) + 1024 * i) = kr[i];
       }
-      if (more) load_values(blk + kPagedWaves);
+      if (j_new < BLK && lane < UPR) *(u32x4*)(smv + j_new * D + ((lane ^ key_swz<D>(j_new)) << 3)) = *(const u32x4*)&rot[0][QR][lane * 8];
+      if (more) there = load_block(kr, (const __bf16*)p.pg.k, blk + kPagedWaves);
+      asm volatile("" ::: "memory");
+      // products with the queries' first terms and with what is left of them, apart: an infinite key element gives its
+      // infinity with the first term, and NaN where the terms differ in sign
+      f32x4 sc[2], rest[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) sc[t] = rest[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(mask >> (16 * t + 4 * quad + i) & 1)) sc[t][i] = -INFINITY;
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[2], q[3];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) kf[t] = *(const bf16x8*)((const char*)smv + (key_read ^ (64 * ks)) + 32 * D * t);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) q[i] = *(const bf16x8*)&rot[i][q_row][32 * ks + 8 * quad];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          rest[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t], q[2], rest[t], 0, 0, 0);
+          sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t], q[0], sc[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) rest[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t], q[1], rest[t], 0, 0, 0);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) short_settle(sc[t], rest[t]);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < NV; ++i) *(u32x4*)((char*)smv + (value_write ^ value_step(i)) + 1024 * i) = vr[i];
+      if (stored != 0xffffffffu) {                     // rows that are not there weigh 0: their values have to be finite
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (!(stored >> (RPI * i + lane / UPR) & 1)) *(u32x4*)((char*)smv + (value_write ^ value_step(i)) + 1024 * i) = u32x4{0u, 0u, 0u, 0u};
+        asm volatile("" ::: "memory");
+        if (j_new < BLK && lane < UPR) *(u32x4*)(smv + j_new * D + ((lane ^ short_v_swz<D>(j_new)) << 3)) = newest;
+      }
+      if (more) load_block(vr, (const __bf16*)p.pg.v, blk + kPagedWaves);
+      if (mask != 0xffffffffu) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(mask >> (16 * t + 4 * quad + i) & 1)) sc[t][i] = -INFINITY;
+      }
       if (scores && r16 < na) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) *(f32x4*)(scores + j0 + 16 * t + 4 * quad) = sc[t];
@@ -457,7 +541,23 @@ __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(Pag
       u32x4 pw[3];
       const float alpha = short_softmax(sc, mrow, lrow, pw);
       asm volatile("" ::: "memory");
-      short_weigh<D, CAREFUL>(smv, pw, alpha, lane, o);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const char* at = (const char*)smv + (value_read ^ (32 * db));
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)at);
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 32 * D));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[db][i] *= alpha;
+        f32x4 small = CAREFUL ? f32x4{0.f, 0.f, 0.f, 0.f} : o[db];
+        small = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[2]), small, 0, 0, 0);
+        small = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[1]), small, 0, 0, 0);
+        if (CAREFUL) {
+          o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[0]), o[db], 0, 0, 0);
+          short_settle(o[db], small);
+        } else o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[0]), small, 0, 0, 0);
+      }
       asm volatile("" ::: "memory");
     }
   };
@@ -490,60 +590,63 @@ __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_mfma_kernel(Pag
       for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(f, tile[w].o[a][e + j], x[j]);
     }
     finish_group<__bf16, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, e, m, l, x);
+    if (e == 0) states[a] = f32x2{m, 1.f / l};
   }
+  if (p.scores && !p.part_o) add_weights(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
 }
 
-// Joins the splits' states: block x = 0 of a (kv head, stream) the outputs, the others 1024 rows' weights each.
-constexpr int kJoinRows = 1024;
+// Joins the splits' states.  Blocks x < Hq / Hkv of a (kv head, stream) give one query head's output each: 256 / (D / 8) lanes
+// share the splits, then meet in LDS.  The blocks behind them give 1024 rows' weights each.
+constexpr int kJoinThreads = kPagedThreads, kMaxGroup = 128;
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
-  constexpr int LPK = D / 8;
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p) {
+  constexpr int LPK = D / 8, LANES = kJoinThreads / LPK;
   const int c = blockIdx.y, u = blockIdx.z, gq = p.hq / p.hkv, tid = threadIdx.x;
   const int n = length_of(p.cache_len, u, p.max_len, p.pg);
   if (n < 0) return;
   const int used = (n + p.chunk) / p.chunk;    // splits that have rows: n + 1 rows
   const long long head0 = (long long)u * p.hq + c * gq;
-  if (blockIdx.x == 0) {
-    for (int i = tid; i < gq * LPK; i += 256) {
-      const int a = i / LPK, sb = i % LPK;
-      float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int z = 0; z < used; ++z) {
-        const long long slot = (head0 + a) * p.n_splits + z;
-        float x2[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x2[e] = p.part_o[slot * D + sb * 8 + e];
-        merge_state<8>(m, l, x, p.part_ml[slot * 2], p.part_ml[slot * 2 + 1], x2);
-      }
-      const float inv = 1.f / l;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= inv;
-      Row8<T>::store((T*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a)) * D + sb * 8, x);
+  if ((int)blockIdx.x < gq) {
+    const int a = blockIdx.x, sb = tid % LPK, part = tid / LPK;
+    __shared__ float sm[LANES][LPK][10];
+    float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int z = part; z < used; z += LANES) {
+      const long long slot = (head0 + a) * p.n_splits + z;
+      const f32x4 lo = *(const f32x4*)(p.part_o + slot * D + sb * 8), hi = *(const f32x4*)(p.part_o + slot * D + sb * 8 + 4);
+      const f32x2 state = *(const f32x2*)(p.part_ml + slot * 2);
+      const float x2[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      merge_state<8>(m, l, x, state[0], state[1], x2);
     }
+    sm[part][sb][0] = m;
+    sm[part][sb][1] = l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sm[part][sb][2 + e] = x[e];
+    __syncthreads();
+    if (part > 0) return;
+    for (int i = 1; i < min(LANES, used); ++i) merge_state<8>(m, l, x, sm[i][sb][0], sm[i][sb][1], &sm[i][sb][2]);
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    Row8<T>::store((T*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a)) * D + sb * 8, x);
     return;
   }
-  const int j0 = (int)(blockIdx.x - 1) * kJoinRows, j1 = min(min(n + 1, j0 + kJoinRows), p.w_cap);
+  const int j0 = (int)(blockIdx.x - gq) * kWeightRows, j1 = min(min(n + 1, j0 + kWeightRows), p.w_cap);
   if (j0 >= j1) return;
-  __shared__ float ref[128], inv[128];
-  for (int a = tid; a < min(gq, 128); a += 256) {
-    float m = -INFINITY, l = 0.f;
-    for (int z = 0; z < used; ++z) m = fmaxf(m, p.part_ml[((head0 + a) * p.n_splits + z) * 2]);
-    for (int z = 0; z < used; ++z) {
-      const float mz = p.part_ml[((head0 + a) * p.n_splits + z) * 2], lz = p.part_ml[((head0 + a) * p.n_splits + z) * 2 + 1];
-      l += mz == -INFINITY ? lz : lz * __builtin_amdgcn_exp2f(mz - m);
+  __shared__ f32x2 state[kMaxGroup];
+  add_weights(p, u, c, n, j0, j1, state, [&]() {
+    for (int a = tid / kWave; a < gq; a += kJoinThreads / kWave) {   // a wave per head
+      const f32x2* split = (const f32x2*)p.part_ml + (head0 + a) * p.n_splits;
+      float m = -INFINITY, l = 0.f;
+      for (int z = tid % kWave; z < used; z += kWave) merge_state<0>(m, l, nullptr, split[z][0], split[z][1], nullptr);
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const float m2 = __shfl_xor(m, o, kWave), l2 = __shfl_xor(l, o, kWave);
+        merge_state<0>(m, l, nullptr, m2, l2, nullptr);
+      }
+      if (tid % kWave == 0) state[a] = f32x2{m, 1.f / l};
     }
-    ref[a] = m;
-    inv[a] = 1.f / l;
-  }
-  __syncthreads();
-  const long long to = ((long long)u * p.hkv + c) * p.w_cap;
-  for (int j = j0 + tid; j < j1; j += 256) {
-    float w = 0.f;
-    for (int a = 0; a < gq; ++a) {
-      const float s = p.scores[(head0 + a) * p.score_stride + j];
-      w += s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - ref[a]) * inv[a];
-    }
-    p.w_out[to + j] = (j < n && p.w_in ? p.w_in[to + j] : 0.f) + w;
-  }
+    __syncthreads();
+  });
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -706,17 +809,32 @@ int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v,
 
 struct PagedPlan { int n_splits, chunk, score_stride; size_t part_o, part_ml, scores; };
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+// query heads that a workgroup serves, and the workgroups of a group of heads
+static int paged_heads(const earn_attn_desc* desc) {
+  const int gq = desc->n_q_heads / desc->n_kv_heads;
+  if (desc->dtype == EARN_BF16) return gq > 8 ? 16 : 8;
+  return gq > 4 ? 8 : gq > 2 ? 4 : gq;
+}
+static int paged_parts(const earn_attn_desc* desc) {
+  const int gq = desc->n_q_heads / desc->n_kv_heads, heads = paged_heads(desc);
+  return (gq + heads - 1) / heads;
+}
 static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
   PagedPlan pl{};
   const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
-  long long splits = (1024 + pairs - 1) / pairs;
-  if (splits > (rows + 255) / 256) splits = (rows + 255) / 256;
-  if (splits < (rows + kPagedMaxChunk - 1) / kPagedMaxChunk) splits = (rows + kPagedMaxChunk - 1) / kPagedMaxChunk;
-  pl.chunk = (int)(((rows + splits - 1) / splits + 63) / 64 * 64);
+  const int forced = tuning(kTunePagedChunk, 0);
+  long long chunk = rows * pairs / 4096;
+  if (chunk < 256) chunk = 256;
+  if (rows <= 640) chunk = rows;
+  if (forced > 0) chunk = forced;
+  if (chunk > kPagedMaxChunk) chunk = kPagedMaxChunk;
+  if (chunk > rows) chunk = rows;
+  pl.chunk = (int)((chunk + 63) / 64 * 64);
   pl.n_splits = (int)((rows + pl.chunk - 1) / pl.chunk);
   pl.score_stride = (int)((rows + 31) / 32 * 32);   // whole blocks of rows
   const size_t heads = (size_t)n_streams * desc->n_q_heads;
-  if (pl.n_splits > 1 || weights) {
+  // without splits, and with all heads of a group in one workgroup, that workgroup finishes weights and outputs by itself
+  if (pl.n_splits > 1 || (weights && paged_parts(desc) > 1)) {
     pl.part_o = up256(heads * pl.n_splits * desc->head_dim * 4);
     pl.part_ml = up256(heads * pl.n_splits * 8);
   }
@@ -748,13 +866,20 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   const int rc = make_head_map(desc, &p.heads, "earn_decode_attn_paged");
   if (rc != EARN_OK) return rc;
   const bool mfma = desc->dtype == EARN_BF16;
-  const int gq = p.hq / p.hkv, g = mfma ? (gq > 8 ? 16 : 8) : gq > 4 ? 8 : gq > 2 ? 4 : gq, parts = (gq + g - 1) / g;
-  const dim3 grid(pl.n_splits, p.hkv * parts, n_streams);
+  // Values that the caches in front of the memory (256 MB) cannot hold until the next step are loaded without a place there: 16
+  // streams of 8192-32768 rows 237 -> 217 us; 256 streams of 100-500 rows, 63 MB, 19.2 -> 19.6.
+  const bool streamed = 2ll * n_streams * p.hkv * max_len * desc->head_dim * (mfma ? 2 : 4) > (256ll << 20);
+  const int gq = p.hq / p.hkv, g = paged_heads(desc), parts = paged_parts(desc);
+  // splits last: consecutive workgroups go to the XCDs in turn, and with two splits side by side every other XCD had short ones only
+  // (64 streams of 256-2080 rows, 32 heads, two splits: 277 us, this way 209)
+  const dim3 grid(p.hkv * parts, n_streams, pl.n_splits);
   for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
-    if (mfma && g == 8) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (mfma) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16>), grid, dim3(kPagedThreads), 0, stream, p);
+    if (mfma && g == 8 && streamed) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8, true>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (mfma && g == 8) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8, false>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (mfma && streamed) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16, true>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if (mfma) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16, false>), grid, dim3(kPagedThreads), 0, stream, p);
     else if constexpr (sizeof(T) == 2) return;
     else if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
     else if (g == 2) hipLaunchKernelGGL((paged_decode_kernel<T, D, 2>), grid, dim3(kPagedThreads), 0, stream, p);
@@ -765,8 +890,8 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
     {
-      const int row_blocks = w_out ? (int)(((long long)max_len + kJoinRows) / kJoinRows) : 0;
-      hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(1 + row_blocks, p.hkv, n_streams), dim3(256), 0, stream, p);
+      const int row_blocks = w_out ? (int)(((long long)max_len + kWeightRows) / kWeightRows) : 0;
+      hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(gq + row_blocks, p.hkv, n_streams), dim3(kJoinThreads), 0, stream, p);
     }
   });
   return launched();
