@@ -37,30 +37,49 @@ __device__ __forceinline__ int capacity_of(const Pages& pg) {   // rows that a t
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// store: 16 bytes of a K and a V row per thread
+// store: 4 times 16 bytes of a K and a V row per thread
 // ------------------------------------------------------------------------------------------------------------------
+constexpr int kStoreUnits = 4;
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_store_kernel(const T* __restrict__ k, const T* __restrict__ v, Pages pg,
+__global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restrict__ k, const u32x4* __restrict__ v, Pages pg,
                                                           const int32_t* __restrict__ cu, const int32_t* __restrict__ start,
-                                                          int batch, int total) {
+                                                          int batch, int total, FastDiv by_heads) {
   constexpr int UPR = D * (int)sizeof(T) / 16;   // 16-byte units of a row
-  const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long row = t / UPR;                 // (token, kv head)
-  const int unit = (int)(t % UPR);
-  const int token = (int)(row / pg.hkv), c = (int)(row % pg.hkv);
-  if (token >= total) return;
-  const int s = find_seq(cu, batch, token);
-  int b0, n;
-  clamped_bounds(cu, s, total, total, b0, n);
-  if (token < b0 || token >= b0 + n) return;     // behind the last sequence
-  const long long r = (long long)(token - b0) + (start ? start[s] : 0);
-  if (r < 0 || r >= capacity_of(pg)) return;
-  int in_page;
-  const int page = page_of_row(pg, s, (int)r, in_page);
-  if (page < 0) return;
-  const long long to = row_offset<D>(pg, page, c, in_page) * (long long)sizeof(T) / 16 + unit;
-  ((u32x4*)pg.k)[to] = ((const u32x4*)k)[t];
-  ((u32x4*)pg.v)[to] = ((const u32x4*)v)[t];
+  constexpr int STEP = 256 / UPR;                // rows (token, kv head) of 256 units
+  const int unit = threadIdx.x % UPR;
+  const long long row0 = (long long)blockIdx.x * (STEP * kStoreUnits) + threadIdx.x / UPR, rows = (long long)total * pg.hkv;
+  u32x4 x[kStoreUnits], y[kStoreUnits];
+  long long to[kStoreUnits];
+#pragma unroll
+  for (int i = 0; i < kStoreUnits; ++i) {
+    const long long row = row0 + i * STEP;
+    to[i] = -1;
+    if (row >= rows) continue;
+    x[i] = __builtin_nontemporal_load(k + row * UPR + unit);
+    y[i] = __builtin_nontemporal_load(v + row * UPR + unit);
+  }
+#pragma unroll
+  for (int i = 0; i < kStoreUnits; ++i) {
+    const long long row = row0 + i * STEP;
+    if (row >= rows) continue;
+    const int token = rows < 0x7fffffff ? (int)by_heads.div((unsigned)row) : (int)(row / pg.hkv);
+    const int c = (int)(row - (long long)token * pg.hkv);
+    const int s = find_seq(cu, batch, token);
+    int b0, n;
+    clamped_bounds(cu, s, total, total, b0, n);
+    if (token < b0 || token >= b0 + n) continue;   // behind the last sequence
+    const long long r = (long long)(token - b0) + (start ? start[s] : 0);
+    if (r < 0 || r >= capacity_of(pg)) continue;
+    int in_page;
+    const int page = page_of_row(pg, s, (int)r, in_page);
+    if (page >= 0) to[i] = row_offset<D>(pg, page, c, in_page) * (long long)sizeof(T) / 16 + unit;
+  }
+#pragma unroll
+  for (int i = 0; i < kStoreUnits; ++i) {
+    if (to[i] < 0) continue;
+    ((u32x4*)pg.k)[to[i]] = x[i];
+    ((u32x4*)pg.v)[to[i]] = y[i];
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -610,12 +629,22 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p)
     const int a = blockIdx.x, sb = tid % LPK, part = tid / LPK;
     __shared__ float sm[LANES][LPK][10];
     float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int z = part; z < used; z += LANES) {
-      const long long slot = (head0 + a) * p.n_splits + z;
-      const f32x4 lo = *(const f32x4*)(p.part_o + slot * D + sb * 8), hi = *(const f32x4*)(p.part_o + slot * D + sb * 8 + 4);
-      const f32x2 state = *(const f32x2*)(p.part_ml + slot * 2);
-      const float x2[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      merge_state<8>(m, l, x, state[0], state[1], x2);
+    for (int z0 = part; z0 < used; z0 += 4 * LANES) {   // four splits' states on their way together
+      f32x4 x2[4][2];
+      f32x2 state[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const long long slot = (head0 + a) * p.n_splits + min(z0 + i * LANES, used - 1);
+        state[i] = *(const f32x2*)(p.part_ml + slot * 2);
+        x2[i][0] = *(const f32x4*)(p.part_o + slot * D + sb * 8);
+        x2[i][1] = *(const f32x4*)(p.part_o + slot * D + sb * 8 + 4);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (z0 + i * LANES >= used) continue;
+        const float y[8] = {x2[i][0][0], x2[i][0][1], x2[i][0][2], x2[i][0][3], x2[i][1][0], x2[i][1][1], x2[i][1][2], x2[i][1][3]};
+        merge_state<8>(m, l, x, state[i][0], state[i][1], y);
+      }
     }
     sm[part][sb][0] = m;
     sm[part][sb][1] = l;
@@ -623,6 +652,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p)
     for (int e = 0; e < 8; ++e) sm[part][sb][2 + e] = x[e];
     __syncthreads();
     if (part > 0) return;
+#pragma unroll 4
     for (int i = 1; i < min(LANES, used); ++i) merge_state<8>(m, l, x, sm[i][sb][0], sm[i][sb][1], &sm[i][sb][2]);
     const float inv = 1.f / l;
 #pragma unroll
@@ -661,17 +691,66 @@ struct EvictParams {
   int n_streams, max_len, w_cap, w_out_cap, budget, first, last, new_pages;
 };
 
-// a weight as an integer of the same order: NaN below everything, zeros of either sign equal
+// a weight as an integer of the same order: NaN below everything, zeros of either sign equal; 0 is no weight's
 __device__ __forceinline__ unsigned weight_key(float w) {
-  if (w != w) return 0u;
+  if (w != w) return 1u;
   const unsigned b = __float_as_uint(w == 0.f ? 0.f : w);
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// One workgroup per (kv head, stream): the key of the last row that is kept by weight, bit by bit from the top, then the kept
-// rows in their order.  A wave has a run of rows of its own.
+// One workgroup per (kv head, stream): the key of the last row that is kept by weight, 11, 11 and 10 bits of it at a time from
+// histograms of the rows that agree so far, then the kept rows in their order.  A wave has a run of rows of its own, ROWS / 16 of
+// them, whose keys stay in registers (ROWS = 0: any number, read again in every pass).  Weights crowd: most of the first histogram's
+// additions go to a few neighbouring bins, so that eight copies of it, a lane's by its number, take them in turn.  The rows
+// that agree in the first 11 bits are listed, a few hundred as a rule, and the other digits come from the list.  One workgroup
+// does all of it, so what bounds it is how often it touches every row: the first histogram, the list, two counts, the result.
+constexpr int kDigitBins = 2048, kDigitCopies = 8, kDigitList = 4096;
+struct SelectSmem {
+  int bins[kDigitBins * kDigitCopies];
+  unsigned list[kDigitList];
+  int wave_sum[kSelectWaves], wave_above[kSelectWaves], wave_equal[kSelectWaves];
+  int digit, above, in_bin, listed;
+};
+// The bin, from the top, in which the need-th entry lies (need >= 1, at most all entries); `above`: entries in higher bins, `in_bin`:
+// in this one.
+template <int COPIES>
+__device__ __forceinline__ int select_digit(SelectSmem& sm, int need, int& above, int& in_bin) {
+  constexpr int PER = kDigitBins / kSelectThreads;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int count[PER], all = 0;                       // this thread's bins, from the top
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int bin = kDigitBins - 1 - (tid * PER + i);
+    count[i] = 0;
+#pragma unroll
+    for (int k = 0; k < COPIES; ++k) count[i] += sm.bins[bin * COPIES + (k + tid) % COPIES];
+    all += count[i];
+  }
+  int sum = all;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(sum, o, kWave);
+    if (lane >= o) sum += y;
+  }
+  if (lane == kWave - 1) sm.wave_sum[wave] = sum;
+  __syncthreads();
+  int before = sum - all;
+  for (int i = 0; i < wave; ++i) before += sm.wave_sum[i];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < need && before + count[i] >= need) { sm.digit = kDigitBins - 1 - (tid * PER + i); sm.above = before; sm.in_bin = count[i]; }
+    before += count[i];
+  }
+  __syncthreads();
+  above = sm.above;
+  in_bin = sm.in_bin;
+  return sm.digit;
+}
+
+template <int ROWS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
-  __shared__ int counts[kSelectWaves], counts2[kSelectWaves];
+  constexpr int PER = ROWS / kSelectThreads;     // rows of a thread
+  __shared__ SelectSmem sm;
   const int c = blockIdx.x, u = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = length_of(p.cache_len, u, min(p.max_len, p.w_cap), p.pg);
   const long long pair = (long long)u * p.pg.hkv + c;
@@ -689,62 +768,101 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
     return;
   }
   const int lo = p.first, hi = n - p.last, need = p.budget - p.first - p.last;   // rows [lo, hi) compete for `need` places
+  // lane's rows: begin + 64 i + lane
   const int per = ((hi - lo + kSelectWaves - 1) / kSelectWaves + kWave - 1) / kWave * kWave;
   const int begin = lo + wave * per, end = min(hi, begin + per);
-  // (a wave's count of rows whose key satisfies cmp; summed over the workgroup)
-  auto count_all = [&](auto cmp) {
-    int mine = 0;
-    for (int j = begin; j < end; j += kWave) mine += __popcll(__ballot(j + lane < end && cmp(weight_key(w[min(j + lane, end - 1)]))));
-    __syncthreads();
-    if (lane == 0) counts[wave] = mine;
-    __syncthreads();
-    int all = 0;
-    for (int i = 0; i < kSelectWaves; ++i) all += counts[i];
-    return all;
-  };
-  // the largest key t that at least `need` rows reach
-  unsigned t = 0;
-  if (need > 0)
-    for (int bit = 31; bit >= 0; --bit) {
-      const unsigned with = t | 1u << bit;
-      if (count_all([with](unsigned k) { return k >= with; }) >= need) t = with;
-    }
-  const int equal_kept = need - (need > 0 ? count_all([t](unsigned k) { return k > t; }) : 0);
-  // where each wave's equal rows and kept rows begin
-  int above = 0, equal = 0;
-  for (int j = begin; j < end && need > 0; j += kWave) {
-    const unsigned k = weight_key(w[min(j + lane, end - 1)]);
-    above += __popcll(__ballot(j + lane < end && k > t));
-    equal += __popcll(__ballot(j + lane < end && k == t));
+  unsigned held[PER > 0 ? PER : 1];
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) held[i] = __float_as_uint(begin + i * kWave + lane < end ? w[begin + i * kWave + lane] : 0.f);
   }
-  __syncthreads();
-  if (lane == 0) { counts[wave] = above; counts2[wave] = equal; }
-  __syncthreads();
-  int at = p.first, eq = 0;
-  for (int i = 0; i < wave; ++i) { at += counts[i]; eq += counts2[i]; }
-  at += min(eq, equal_kept);
   for (int i = tid; i < p.first; i += kSelectThreads) {
     kept[i] = i;
     if (w_out) w_out[i] = w[i];
-  }
-  for (int j = begin; j < end && need > 0; j += kWave) {
-    const float x = w[min(j + lane, end - 1)];
-    const unsigned k = weight_key(x);
-    const unsigned long long before = (1ull << lane) - 1, is_equal = __ballot(j + lane < end && k == t);
-    const bool keep = j + lane < end && (k > t || (k == t && eq + __popcll(is_equal & before) < equal_kept));
-    const unsigned long long mask = __ballot(keep);
-    if (keep) {
-      const int to = at + __popcll(mask & before);
-      kept[to] = j + lane;
-      if (w_out) w_out[to] = x;
-    }
-    at += __popcll(mask);
-    eq += __popcll(is_equal);
   }
   for (int i = tid; i < p.last; i += kSelectThreads) {
     kept[p.budget - p.last + i] = hi + i;
     if (w_out) w_out[p.budget - p.last + i] = w[hi + i];
   }
+  if (need <= 0) return;
+  for (int i = tid; i < kDigitBins * kDigitCopies / 4; i += kSelectThreads) *(u32x4*)&sm.bins[4 * i] = u32x4{0u, 0u, 0u, 0u};
+  if (tid == 0) sm.listed = 0;
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) held[i] = begin + i * kWave + lane < end ? weight_key(__uint_as_float(held[i])) : 0u;
+  }
+  auto each = [&](auto f) {                      // f(row, key), all lanes of a wave together; key 0 where there is no row
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (begin + i * kWave < end) f(begin + i * kWave + lane, held[i]);
+    } else {
+      for (int j0 = begin; j0 < end; j0 += kWave) f(j0 + lane, j0 + lane < end ? weight_key(w[j0 + lane]) : 0u);
+    }
+  };
+  __syncthreads();
+  each([&](int, unsigned k) { atomicAdd(&sm.bins[(k >> 21) * kDigitCopies + lane % kDigitCopies], 1); });
+  __syncthreads();
+  int above, in_bin;                             // rows whose key exceeds what is known of t, that agree with it
+  unsigned t = (unsigned)select_digit<kDigitCopies>(sm, need, above, in_bin) << 21;
+  const bool listed = in_bin <= kDigitList;
+  if (listed) {                                  // a place in the list for each wave's, then the keys
+    int mine = 0;
+    each([&](int, unsigned k) { mine += __popcll(__ballot(k >> 21 == t >> 21)); });
+    int to = 0;
+    if (lane == 0 && mine) to = atomicAdd(&sm.listed, mine);
+    to = __builtin_amdgcn_readfirstlane(to);
+    each([&](int, unsigned k) {
+      const bool here = k >> 21 == t >> 21;
+      const unsigned long long mask = __ballot(here);
+      if (here) sm.list[to + __popcll(mask & ((1ull << lane) - 1))] = k;
+      to += __popcll(mask);
+    });
+  }
+  const int n_list = in_bin;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    const int shift = pass == 0 ? 10 : 0, known = pass == 0 ? 21 : 10, digit = pass == 0 ? 2047 : 1023;
+    for (int i = tid; i < kDigitBins / 4; i += kSelectThreads) *(u32x4*)&sm.bins[4 * i] = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    auto count = [&](unsigned k) {
+      if ((k ^ t) >> known == 0) atomicAdd(&sm.bins[k >> shift & digit], 1);
+    };
+    if (listed) {
+      for (int i = tid; i < n_list; i += kSelectThreads) count(sm.list[i]);
+    } else {
+      each([&](int, unsigned k) { count(k); });
+    }
+    __syncthreads();
+    int over;
+    t |= (unsigned)select_digit<1>(sm, need - above, over, in_bin) << shift;
+    above += over;
+  }
+  const int equal_kept = need - above;           // of the rows whose key is t, the first ones
+  int mine_above = 0, mine_equal = 0;
+  each([&](int, unsigned k) {
+    mine_above += __popcll(__ballot(k > t));
+    mine_equal += __popcll(__ballot(k == t));
+  });
+  if (lane == 0) { sm.wave_above[wave] = mine_above; sm.wave_equal[wave] = mine_equal; }
+  __syncthreads();
+  int at = p.first, eq = 0;
+  for (int i = 0; i < wave; ++i) { at += sm.wave_above[i]; eq += sm.wave_equal[i]; }
+  at += min(eq, equal_kept);
+  int left = __builtin_amdgcn_readfirstlane(max(equal_kept - eq, 0));   // equal rows that this wave still keeps
+  at = __builtin_amdgcn_readfirstlane(at);
+  each([&](int j, unsigned k) {
+    unsigned long long mask = __ballot(k > t), same = __ballot(k == t);
+    for (int drop = __popcll(same) - left; drop > 0; --drop) same &= ~(1ull << (63 - __builtin_clzll(same)));
+    left -= __popcll(same);
+    mask |= same;
+    if (mask >> lane & 1) {
+      const int to = at + __popcll(mask & ((1ull << lane) - 1));
+      kept[to] = j;
+      if (w_out) w_out[to] = w[j];
+    }
+    at += __popcll(mask);
+  });
 }
 
 // 16 bytes of a K and a V row per thread
@@ -798,11 +916,12 @@ int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v,
                        int total, void* k_pages, void* v_pages, const int32_t* table, int max_pages, int n_pages, int page_size,
                        hipStream_t stream) {
   const Pages pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
-  const long long units = (long long)total * desc->n_kv_heads * (desc->head_dim * (desc->dtype == EARN_F32 ? 4 : 2) / 16);
   for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
-    hipLaunchKernelGGL((paged_store_kernel<T, decltype(d)::value>), dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream,
-                       (const T*)k, (const T*)v, pg, cu, start, batch, total);
+    constexpr int D = decltype(d)::value, rows = 256 / (D * (int)sizeof(T) / 16) * kStoreUnits;   // of a workgroup
+    const long long blocks = ((long long)total * desc->n_kv_heads + rows - 1) / rows;
+    hipLaunchKernelGGL((paged_store_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, stream, (const u32x4*)k, (const u32x4*)v, pg, cu,
+                       start, batch, total, FastDiv::of((unsigned)desc->n_kv_heads));
   });
   return launched();
 }
@@ -906,7 +1025,10 @@ int launch_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages,
   p.cache_len = cache_len; p.w_in = w_in; p.w_out = w_out; p.new_table = new_table; p.kept = kept; p.len_out = len_out;
   p.n_streams = n_streams; p.max_len = max_len; p.w_cap = w_cap; p.w_out_cap = w_out_cap;
   p.budget = budget; p.first = first; p.last = last; p.new_pages = new_pages;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(desc->n_kv_heads, n_streams), dim3(kSelectThreads), 0, stream, p);
+  const dim3 pairs(desc->n_kv_heads, n_streams);
+  if (max_len <= 4096) hipLaunchKernelGGL(evict_select_kernel<4096>, pairs, dim3(kSelectThreads), 0, stream, p);
+  else if (max_len <= 32768) hipLaunchKernelGGL(evict_select_kernel<32768>, pairs, dim3(kSelectThreads), 0, stream, p);
+  else hipLaunchKernelGGL(evict_select_kernel<0>, pairs, dim3(kSelectThreads), 0, stream, p);
   for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value, rows = 256 / (D * (int)sizeof(T) / 16);
