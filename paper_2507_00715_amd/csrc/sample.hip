@@ -10,8 +10,17 @@
 // them as it likes (histograms by atomics, prefix sums in any tree) and every call gives the same token.
 //
 // One workgroup a row.  A wave has a run of the row, 16 bytes a lane and unit, and the row stays in registers (UNITS units; 0:
-// any number, read again in every pass).  Passes: the largest logit; a histogram over (l_max - l) / T; the few entries of the bin in
-// which a beginning ends, ranked among each other; the kept weights' sums by wave, then by unit of the wave that u W falls to.
+// any number, read again in every pass).  What bounds a row is how often every entry is touched, by one CU's vector ALU and
+// LDS, so the passes over all entries are few and short:
+//   - the largest logit;
+//   - top-k up to kSmallK: a histogram over (l_max - l) / T of the largest entry of every 16 bytes gives a border that at least k
+//     entries reach, and few more: those are listed, and the rest happens in the list;
+//   - else top-k: a histogram of all entries; top-p: one of their weights; the few entries of the bin in which a beginning ends are
+//     ranked among each other;
+//   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept),
+//     then by unit of the wave that u W falls to, all waves together.
+#include <type_traits>
+
 #include "common.h"
 
 namespace earn {
@@ -21,6 +30,7 @@ constexpr int kBins = 2048;            // of (l_max - l) / T in steps of 1/64; t
 constexpr int kBinsPerUnit = 64;
 constexpr int kFraction = 44;          // exp(-31.98) 2^44 < 1/2: the last bin's weights are all zero
 constexpr int kListMax = 1024;
+constexpr int kSmallK = 512;           // largest top-k that is worked out in the list
 constexpr int kExpSteps = 128;         // of the table of powers of two
 
 struct SampleParams {
@@ -44,14 +54,14 @@ struct SampleSmem {
   u64 list_w[kListMax];
   u64 list_key[kListMax];        // (order key, ~index): larger is earlier in the order
   double power[kExpSteps];       // 2^(i / kExpSteps)
+  float queue[WAVES][2 * kWave];
   u64 wave_mass[WAVES];
   int wave_count[WAVES];
   float wave_best[WAVES];
   int wave_at[WAVES];
-  int n_list, bin, found_count, found_index, hit_wave;
+  int n_list, bin, found_index, before_count;
   float found_value;
-  u64 before_mass, found_mass, hit_before, hit_total;
-  int before_count;
+  u64 before_mass, found_mass;
 };
 
 template <typename X>
@@ -102,11 +112,11 @@ template <typename T, int UNITS, int WAVES>
 struct Run {
   static constexpr int E = 16 / sizeof(T);
   const T* row;
-  int vocab, begin, n_units, lane;
+  int vocab, units, begin, n_units, lane;   // units: of a wave's run, of the last ones fewer
   bool infinite;                 // the best is +inf: those entries count as 0, all others as -inf
   u32x4 held[UNITS > 0 ? UNITS : 1];
-  __device__ __forceinline__ u32x4 load(int i) const {
-    const int at = begin + (kWave * i + lane) * E;
+  __device__ __forceinline__ u32x4 load(int i) const { return load_at(index(i, 0)); }
+  __device__ __forceinline__ u32x4 load_at(int at) const {
     u32x4 x;
     if (at + E <= vocab) {
       if constexpr (sizeof(T) == 4) x = *(const u32x4_at4*)(row + at);
@@ -127,9 +137,9 @@ struct Run {
   }
   __device__ __forceinline__ void init(const T* row_, int vocab_, int wave, int lane_) {
     row = row_; vocab = vocab_; lane = lane_; infinite = false;
-    const int per = ((vocab + WAVES - 1) / WAVES + kWave * E - 1) / (kWave * E);   // units of a wave
-    begin = min(vocab, wave * per * (kWave * E));
-    n_units = min(per, (vocab - begin + kWave * E - 1) / (kWave * E));
+    units = ((vocab + WAVES - 1) / WAVES + kWave * E - 1) / (kWave * E);
+    begin = min(vocab, wave * units * (kWave * E));
+    n_units = min(units, (vocab - begin + kWave * E - 1) / (kWave * E));
     if constexpr (UNITS > 0) {
 #pragma unroll
       for (int i = 0; i < UNITS; ++i)
@@ -145,7 +155,7 @@ struct Run {
   }
   __device__ __forceinline__ int index(int i, int e) const { return begin + (kWave * i + lane) * E + e; }
   template <typename F>
-  __device__ __forceinline__ void each(F f) const {       // f(entry, logit)
+  __device__ __forceinline__ void each_unit(F f) const {  // f(first entry, unit)
     if constexpr (UNITS > 0) {
 #pragma unroll
       for (int i = 0; i < UNITS; ++i)
@@ -153,104 +163,109 @@ struct Run {
           u32x4 x = held[i];
           int at = index(i, 0);
           asm volatile("" : "+v"(x), "+v"(at));   // opaque: what one pass works out of them is not kept, in registers that there are not, for the next
-#pragma unroll
-          for (int e = 0; e < E; ++e) f(at + e, element(x, e));
+          f(at, x);
         }
     } else {
-      for (int i = 0; i < n_units; ++i) {
-        const u32x4 x = load(i);
-#pragma unroll
-        for (int e = 0; e < E; ++e) f(index(i, e), element(x, e));
-      }
+      for (int i = 0; i < n_units; ++i) f(index(i, 0), load(i));
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {       // f(entry, logit)
+    each_unit([&](int at, const u32x4& x) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f(at + e, element(x, e));
+    });
   }
 };
 
-// A beginning of the order: what comes before the logit `value`, and its equals up to entry `index`; `count` entries that weigh `mass`.
+// A beginning of the order: what comes before the logit `value`, and its equals up to entry `index`; they weigh `mass`.
 struct Beginning {
   float value;
   int index;
   u64 mass;
-  int count;
   __device__ __forceinline__ bool has(int i, float l) const { return l > value || (l == value && i <= index); }
 };
 
-// Does an entry end the beginning that is looked for?  By count: it is the k-th.  By mass: it is the one that reaches the target.
-struct Target {
-  bool by_mass;
-  int k;
-  u64 mass;
-  __device__ __forceinline__ bool hit(int before, u64 mass_before, int n, u64 w) const {
-    return by_mass ? mass_before < mass && mass_before + w >= mass : before < k && before + n >= k;
-  }
-};
-
-// The beginning that `target` ends, from the histogram; called by all threads.  There is one: k is at most the number of entries,
-// the mass at most that of all.
-template <typename R, int WAVES>
-__device__ __forceinline__ Beginning find_beginning(const R& run, const Weights& wt, const Target target, SampleSmem<WAVES>& sm) {
+// The bin in which the k-th entry lies (by sm.count), or the one that reaches `mass` (by sm.mass), and what the bins before it hold;
+// kBins: none.  Called by all threads.
+template <bool BY_MASS, int WAVES>
+__device__ __forceinline__ int find_bin(SampleSmem<WAVES>& sm, int k, u64 mass) {
   constexpr int THREADS = kWave * WAVES, PER = kBins / THREADS;
+  typedef typename std::conditional<BY_MASS, u64, int>::type Sum;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  // the bin that the target ends in
-  int cs = 0;
-  u64 ms = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) { cs += sm.count[PER * tid + i]; ms += sm.mass[PER * tid + i]; }
-  const int cs_in = wave_scan(cs, lane);
-  const u64 ms_in = wave_scan(ms, lane);
+  const Sum target = BY_MASS ? (Sum)mass : (Sum)k;
   __syncthreads();
-  if (lane == kWave - 1) { sm.wave_count[wave] = cs_in; sm.wave_mass[wave] = ms_in; }
-  if (tid == 0) sm.n_list = 0;
-  __syncthreads();
-  int cb = cs_in - cs;
-  u64 mb = ms_in - ms;
-  for (int i = 0; i < wave; ++i) { cb += sm.wave_count[i]; mb += sm.wave_mass[i]; }
+  Sum own[PER], sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int c = sm.count[PER * tid + i];
-    const u64 m = sm.mass[PER * tid + i];
-    if (target.hit(cb, mb, c, m)) { sm.bin = PER * tid + i; sm.before_count = cb; sm.before_mass = mb; }
-    cb += c;
-    mb += m;
+    if constexpr (BY_MASS) own[i] = sm.mass[PER * tid + i]; else own[i] = sm.count[PER * tid + i];
+    sum += own[i];
+  }
+  const Sum upto = wave_scan(sum, lane);
+  if (lane == kWave - 1) { if constexpr (BY_MASS) sm.wave_mass[wave] = upto; else sm.wave_count[wave] = upto; }
+  if (tid == 0) { sm.bin = kBins; sm.n_list = 0; }
+  __syncthreads();
+  Sum before = upto - sum;
+  for (int i = 0; i < wave; ++i) { if constexpr (BY_MASS) before += sm.wave_mass[i]; else before += sm.wave_count[i]; }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < target && before + own[i] >= target) {
+      sm.bin = PER * tid + i;
+      if constexpr (BY_MASS) sm.before_mass = before; else sm.before_count = before;
+    }
+    before += own[i];
   }
   __syncthreads();
-  const int bin = sm.bin, before = sm.before_count;
-  const u64 mass_before = sm.before_mass;
-  if (sm.count[bin] <= kListMax) {
-    run.each([&](int i, float l) {
-      if (l > -INFINITY && wt.bin(l) == bin) {
-        const int at = atomicAdd(&sm.n_list, 1);
-        sm.list_w[at] = wt.of(l);
-        sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
-      }
-    });
-    __syncthreads();
-    const int n = sm.n_list;
+  return sm.bin;
+}
+
+// The beginning that the k-th entry ends, or the first entry at which the weights reach `mass`, of those in `within`; the histogram
+// of these entries is in sm.  There is such an entry.  (The mass of a beginning by count is left to the caller.)  Called by all threads.
+template <bool BY_MASS, typename R, int WAVES>
+__device__ __forceinline__ Beginning find_beginning(const R& run, const Weights& wt, const Beginning& within, int k, u64 mass, SampleSmem<WAVES>& sm) {
+  constexpr int THREADS = kWave * WAVES;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int bin = find_bin<BY_MASS>(sm, k, mass);
+  const int before = BY_MASS ? 0 : sm.before_count;
+  const u64 mass_before = BY_MASS ? sm.before_mass : 0;
+  run.each([&](int i, float l) {
+    if (l > -INFINITY && wt.bin(l) == bin && within.has(i, l)) {
+      const int at = atomicAdd(&sm.n_list, 1);
+      if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
+    }
+  });
+  __syncthreads();
+  const int n = sm.n_list;
+  if (n <= kListMax) {
+    if constexpr (BY_MASS) {
+      for (int a = tid; a < n; a += THREADS) sm.list_w[a] = wt.of(key_value((unsigned)(sm.list_key[a] >> 32)));
+      __syncthreads();
+    }
     for (int a = tid; a < n; a += THREADS) {
       const u64 key = sm.list_key[a];
-      int cnt = before;
-      u64 mass = mass_before;
+      int rank = before;
+      u64 weighed = mass_before;
       for (int b = 0; b < n; ++b) {
         const bool first = sm.list_key[b] > key;
-        cnt += first ? 1 : 0;
-        mass += first ? sm.list_w[b] : 0;
+        if constexpr (BY_MASS) weighed += first ? sm.list_w[b] : 0;
+        else rank += first ? 1 : 0;
       }
-      if (target.hit(cnt, mass, 1, sm.list_w[a])) {
+      const u64 own = BY_MASS ? sm.list_w[a] : 0;
+      if (BY_MASS ? weighed < mass && weighed + own >= mass : rank == k - 1) {
         sm.found_value = key_value((unsigned)(key >> 32));
         sm.found_index = (int)~(unsigned)key;
-        sm.found_count = cnt + 1;
-        sm.found_mass = mass + sm.list_w[a];
+        sm.found_mass = weighed + own;
       }
     }
     __syncthreads();
-    return Beginning{sm.found_value, sm.found_index, sm.found_mass, sm.found_count};
+    return Beginning{sm.found_value, sm.found_index, sm.found_mass};
   }
   // Too many for the list (mostly equal logits): the last key, bit by bit, then its equals in order of their index.
-  auto reach = [&](unsigned key, int& cnt, u64& mass) {   // entries of the bin whose key is at least `key`
+  auto reach = [&](unsigned key, int& cnt, u64& sum) {   // entries of the bin whose key is at least `key`
     int c = 0;
     u64 m = 0;
-    run.each([&](int, float l) {
-      if (l > -INFINITY && wt.bin(l) == bin && order_key(l) >= key) { ++c; m += wt.of(l); }
+    run.each([&](int i, float l) {
+      if (l > -INFINITY && wt.bin(l) == bin && order_key(l) >= key && within.has(i, l)) { ++c; m += BY_MASS ? wt.of(l) : 0; }
     });
     c = wave_sum(c);
     m = wave_sum(m);
@@ -258,23 +273,22 @@ __device__ __forceinline__ Beginning find_beginning(const R& run, const Weights&
     if (lane == 0) { sm.wave_count[wave] = c; sm.wave_mass[wave] = m; }
     __syncthreads();
     cnt = before;
-    mass = mass_before;
-    for (int i = 0; i < WAVES; ++i) { cnt += sm.wave_count[i]; mass += sm.wave_mass[i]; }
+    sum = mass_before;
+    for (int i = 0; i < WAVES; ++i) { cnt += sm.wave_count[i]; sum += sm.wave_mass[i]; }
   };
   unsigned t = 0;
   int cnt;
-  u64 mass;
+  u64 sum;
 #pragma unroll 1
-  for (int bit = 31; bit >= 0; --bit) {
-    const unsigned with = t | 1u << bit;
-    reach(with, cnt, mass);
-    if (target.by_mass ? mass >= target.mass : cnt >= target.k) t = with;
+  for (int bit = 31; bit >= -1; --bit) {          // the last round: what comes before the equals (t is a finite float's key)
+    const unsigned with = bit >= 0 ? t | 1u << bit : t + 1;
+    reach(with, cnt, sum);
+    if (bit >= 0 && (BY_MASS ? sum >= mass : cnt >= k)) t = with;
   }
-  reach(t + 1, cnt, mass);                        // what comes before the equals (t is a finite float's key)
   const float value = key_value(t);
-  const u64 each_mass = wt.of(value);
+  const u64 each_mass = BY_MASS ? wt.of(value) : 0;
   // the r-th equal one is the last
-  const int r = target.by_mass ? (int)((target.mass - mass + each_mass - 1) / each_mass) : target.k - cnt;
+  const int r = BY_MASS ? (int)((mass - sum + each_mass - 1) / each_mass) : k - cnt;
   int mine = 0;
   run.each([&](int, float l) { mine += l == value ? 1 : 0; });
   mine = wave_sum(mine);
@@ -298,7 +312,92 @@ __device__ __forceinline__ Beginning find_beginning(const R& run, const Weights&
     }
   }
   __syncthreads();
-  return Beginning{value, sm.found_index, mass + (u64)r * each_mass, cnt + r};
+  return Beginning{value, sm.found_index, sum + (u64)r * each_mass};
+}
+
+// Sum over the workgroup, in every thread.
+template <int WAVES>
+__device__ __forceinline__ u64 block_sum(u64 x, SampleSmem<WAVES>& sm) {
+  x = wave_sum(x);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) sm.wave_mass[threadIdx.x / kWave] = x;
+  __syncthreads();
+  x = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) x += sm.wave_mass[i];
+  return x;
+}
+
+// What the threads need of the row's parameters to finish it.
+struct Draw { double u, temperature; float top_p; double least; int top_k; };
+// u W falls to the first sum that reaches this
+__device__ __forceinline__ u64 reach_of(double u, u64 total) { return min((u64)(u * (double)total) + 1, total); }
+__device__ __forceinline__ float logprob_of(float l, float best, double temperature, u64 total) {
+  const double z = l == best ? 0.0 : ((double)l - (double)best) / temperature;
+  return (float)(z - log((double)total * (1.0 / (double)(1ull << kFraction))));
+}
+
+// Top-k with the rest in the list: its n entries hold the first k.  Four threads an entry share the others.
+template <int WAVES>
+__device__ __forceinline__ void draw_from_list(const SampleParams& p, const Weights& wt, const Draw& d, int n, SampleSmem<WAVES>& sm) {
+  constexpr int THREADS = kWave * WAVES;
+  const int tid = threadIdx.x, part = tid % 4, r = blockIdx.x;
+  auto quad = [](auto x) { x += __shfl_xor(x, 1, kWave); return x + __shfl_xor(x, 2, kWave); };
+  for (int a = tid; a < n; a += THREADS) sm.list_w[a] = wt.of(key_value((unsigned)(sm.list_key[a] >> 32)));
+  __syncthreads();
+  constexpr int SLOTS = kListMax * 4 / THREADS;   // entries of a thread: a = tid / 4 + THREADS / 4 * slot
+  int rank[SLOTS];
+  u64 before[SLOTS], first_k = 0;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int a = tid / 4 + THREADS / 4 * s;
+    rank[s] = 0x7fffffff;
+    before[s] = 0;
+    if (THREADS / 4 * s >= n) continue;
+    const u64 key = a < n ? sm.list_key[a] : 0;
+    int count = 0;
+    u64 sum = 0;
+    for (int b = part; b < n; b += 4) {
+      const bool first = sm.list_key[b] > key;
+      count += first ? 1 : 0;
+      sum += first ? sm.list_w[b] : 0;
+    }
+    count = quad(count);
+    before[s] = quad(sum);
+    if (a < n) rank[s] = count;
+    if (part == 0 && rank[s] < d.top_k) first_k += sm.list_w[a];
+  }
+  first_k = block_sum(first_k, sm);
+  const u64 need = d.top_p < 1.f ? min(max((u64)ceil((double)d.top_p * (double)first_k), (u64)1), first_k) : ~0ull;
+  u64 total = 0;
+  int count = 0;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int a = tid / 4 + THREADS / 4 * s;
+    if (a >= n || part != 0) continue;
+    const float l = key_value((unsigned)(sm.list_key[a] >> 32));
+    const bool keep = rank[s] < d.top_k && before[s] < need && wt.real(l) >= d.least;
+    if (!keep) sm.list_w[a] = 0;                  // (an entry of its own: no one else reads it before the next barrier)
+    total += keep ? sm.list_w[a] : 0;
+    count += keep ? 1 : 0;
+  }
+  total = block_sum(total, sm);
+  count = (int)block_sum((u64)count, sm);
+  const u64 reach = reach_of(d.u, total);
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int a = tid / 4 + THREADS / 4 * s;
+    if (THREADS / 4 * s >= n) continue;
+    const u64 key = a < n ? sm.list_key[a] : 0;
+    u64 sum = 0;
+    for (int b = part; b < n; b += 4) sum += (unsigned)sm.list_key[b] > (unsigned)key ? sm.list_w[b] : 0;   // lower indices
+    sum = quad(sum);
+    if (a < n && part == 0 && sum < reach && sum + sm.list_w[a] >= reach) {
+      p.token[r] = (int)~(unsigned)key;
+      if (p.logprob) p.logprob[r] = logprob_of(key_value((unsigned)(key >> 32)), wt.best, d.temperature, total);
+      if (p.n_kept) p.n_kept[r] = count;
+    }
+  }
 }
 
 template <typename T, int UNITS, int WAVES>
@@ -349,103 +448,147 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   wt.scale = kExpSteps * 1.4426950408889634074 / (double)temperature;
   wt.bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
   wt.power = sm.power;
-  const bool by_mass = top_p < 1.f;
-  Beginning kept{-INFINITY, -1, 0, 0};
-  if (top_k > 0 || by_mass) {
-    u64 all = 0;
+  const Draw d{(double)u, (double)temperature, top_p, min_p > 0.f ? (double)fminf(min_p, 1.f) : 0.0, top_k};
+  typedef Run<T, UNITS, WAVES> R;
+  Beginning kept{-INFINITY, -1, 0};
+  bool limited = false;
+  if (top_k > 0) {
+    if (top_k <= kSmallK) {
+      run.each_unit([&](int, const u32x4& x) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < R::E; ++e) most = fmaxf(most, run.element(x, e));
+        if (most > -INFINITY) atomicAdd(&sm.count[wt.bin(most)], 1);
+      });
+      const int bin = find_bin<false>(sm, top_k, 0);
+      if (bin < kBins - 1) {
+        run.each([&](int i, float l) {
+          if (wt.bin(l) <= bin) {
+            const int at = atomicAdd(&sm.n_list, 1);
+            if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
+          }
+        });
+        __syncthreads();
+        const int n = sm.n_list;
+        if (n <= kListMax) { draw_from_list(p, wt, d, n, sm); return; }
+      }
+      // too few groups, too many equal entries, or far ones: all entries count
+      __syncthreads();
+      for (int i = tid; i < kBins; i += THREADS) sm.count[i] = 0;
+      __syncthreads();
+    }
     int n_finite = 0;
     run.each([&](int, float l) {
-      if (l > -INFINITY) {
-        const int b = wt.bin(l);
-        atomicAdd(&sm.count[b], 1);
-        ++n_finite;
-        if (by_mass && b < kBins - 1) {
-          const u64 w = wt.of(l);
-          atomicAdd(&sm.mass[b], w);
-          all += w;
-        }
+      if (l > -INFINITY) { atomicAdd(&sm.count[wt.bin(l)], 1); ++n_finite; }
+    });
+    limited = block_sum((u64)n_finite, sm) > (u64)top_k;
+    if (limited) kept = find_beginning<false, R, WAVES>(run, wt, kept, top_k, 0, sm);
+  }
+  if (top_p < 1.f) {
+    u64 all = 0;
+    run.each([&](int i, float l) {
+      const int b = wt.bin(l);
+      if (b < kBins - 1 && kept.has(i, l)) {
+        const u64 w = wt.of(l);
+        atomicAdd(&sm.mass[b], w);
+        all += w;
       }
     });
-    all = wave_sum(all);
-    n_finite = wave_sum(n_finite);
-    if (lane == 0) { sm.wave_mass[wave] = all; sm.wave_count[wave] = n_finite; }
-    __syncthreads();
-    all = 0;
-    n_finite = 0;
-    for (int i = 0; i < WAVES; ++i) { all += sm.wave_mass[i]; n_finite += sm.wave_count[i]; }
-    kept.mass = all;
-#pragma unroll 1
-    for (int which = top_k > 0 && top_k < n_finite ? 0 : 1; which < (by_mass ? 2 : 1); ++which) {
-      const double least_mass = ceil((double)top_p * (double)kept.mass);
-      const Target target{which == 1, top_k, which == 1 ? min(max((u64)least_mass, (u64)1), kept.mass) : 0};
-      const Beginning b = find_beginning<Run<T, UNITS, WAVES>, WAVES>(run, wt, target, sm);
-      if (which == 0 || b.value > kept.value || (b.value == kept.value && b.index < kept.index)) kept = b;
-    }
+    all = block_sum(all, sm);
+    kept = find_beginning<true, R, WAVES>(run, wt, kept, 0, min(max((u64)ceil((double)top_p * (double)all), (u64)1), all), sm);
+    limited = true;
   }
-  const double least = min_p > 0.f ? (double)fminf(min_p, 1.f) : 0.0;
-  auto weight = [&](int i, float l, bool& in) {
-    in = kept.has(i, l);
-    u64 w = 0;
-    if (in) {
-      const double x = wt.real(l);
-      in = x >= least;
-      w = in ? Weights::whole(x) : 0;
-    }
-    return w;
+  auto weight = [&](float l, bool& in) {          // of an entry of the beginning
+    const double x = wt.real(l);
+    in = x >= d.least;
+    return in ? Weights::whole(x) : (u64)0;
   };
   // the kept weights of each wave's run
   u64 mine = 0;
   int count = 0;
-  run.each([&](int i, float l) {
-    bool in;
-    mine += weight(i, l, in);
-    count += in ? 1 : 0;
-  });
+  if (limited) {                                  // few entries, as a rule: gathered before their weights are worked out
+    float* queue = sm.queue[wave];
+    int waiting = 0;
+    auto take = [&](int n) {                      // the first n <= 64 of the queue
+      bool in;
+      const u64 w = weight(queue[lane], in);
+      if (lane < n) { mine += w; count += in ? 1 : 0; }
+    };
+    run.each([&](int i, float l) {
+      const bool has = kept.has(i, l);
+      const unsigned long long who = __ballot(has);
+      if (who == 0) return;
+      if (has) queue[waiting + __popcll(who & ((1ull << lane) - 1))] = l;
+      asm volatile("" ::: "memory");              // the wave's LDS operations complete in order: only the compiler has to keep theirs
+      waiting += __popcll(who);
+      if (waiting >= kWave) {
+        take(kWave);
+        const float rest = queue[kWave + lane];
+        asm volatile("" ::: "memory");
+        queue[lane] = rest;
+        asm volatile("" ::: "memory");
+        waiting -= kWave;
+      }
+    });
+    if (waiting > 0) take(waiting);
+  } else {
+    run.each([&](int, float l) {
+      if (l > -INFINITY) {
+        bool in;
+        mine += weight(l, in);
+        count += in ? 1 : 0;
+      }
+    });
+  }
   mine = wave_sum(mine);
   count = wave_sum(count);
   __syncthreads();
   if (lane == 0) { sm.wave_mass[wave] = mine; sm.wave_count[wave] = count; }
   __syncthreads();
-  u64 total = 0, before = 0;
+  u64 total = 0;
   count = 0;
-  for (int i = 0; i < WAVES; ++i) {
-    if (i < wave) before += sm.wave_mass[i];
-    total += sm.wave_mass[i];
-    count += sm.wave_count[i];
-  }
-  // the lowest index whose sum exceeds u W: the sum reaches floor(u W) + 1, at most W
-  const u64 reach = min((u64)((double)u * (double)total) + 1, total);
-  if (before < reach && before + mine >= reach) {
-    for (int i = 0; i < run.n_units; ++i) {
-      const u32x4 x = run.load(i);
-      u64 w[Run<T, UNITS, WAVES>::E], sum = 0;
+  for (int i = 0; i < WAVES; ++i) { total += sm.wave_mass[i]; count += sm.wave_count[i]; }
+  const u64 reach = reach_of(d.u, total);
+  u64 before = 0;
+  int hit = 0;                                    // the wave whose run holds the token
+  while (before + sm.wave_mass[hit] < reach) before += sm.wave_mass[hit++];
+  const int first = hit * run.units * (kWave * R::E);
+  for (int i0 = 0; i0 < run.units; i0 += WAVES) {  // its units, one a wave
+    const int at = first + (kWave * (i0 + wave) + lane) * R::E;
+    u64 w[R::E], sum = 0;
+    u32x4 x = u32x4{0u, 0u, 0u, 0u};
+    if (i0 + wave < run.units) {
+      x = run.load_at(at);
 #pragma unroll
-      for (int e = 0; e < run.E; ++e) {
-        bool in;
-        w[e] = weight(run.index(i, e), run.element(x, e), in);
+      for (int e = 0; e < R::E; ++e) {
+        const float l = run.element(x, e);
+        bool in = false;
+        w[e] = at + e < p.vocab && kept.has(at + e, l) ? weight(l, in) : 0;
         sum += w[e];
       }
-      const u64 upto = before + wave_scan(sum, lane);
-      const unsigned long long hit = __ballot(upto >= reach);
-      if (hit) {
-        if (lane == __ffsll((long long)hit) - 1) {
-          u64 at = upto - sum;
-          bool done = false;
-#pragma unroll
-          for (int e = 0; e < run.E; ++e) {
-            at += w[e];
-            if (!done && at >= reach) {
-              const float l = run.element(x, e);
-              const double z = l == best ? 0.0 : ((double)l - (double)best) / (double)temperature;
-              finish(run.index(i, e), (float)(z - log((double)total * (1.0 / (double)(1ull << kFraction)))), count);
-              done = true;
-            }
-          }
-        }
-        break;
-      }
-      before = __shfl(upto, kWave - 1, kWave);
     }
+    const u64 upto = wave_scan(sum, lane);
+    __syncthreads();
+    if (lane == kWave - 1) sm.wave_mass[wave] = upto;
+    __syncthreads();
+    u64 mine_before = before;
+    for (int i = 0; i < WAVES; ++i) {
+      if (i < wave) mine_before += sm.wave_mass[i];
+      before += sm.wave_mass[i];
+    }
+    u64 so_far = mine_before + upto - sum;
+    if (so_far < reach && so_far + sum >= reach) {   // one lane of one wave
+      bool done = false;
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) {
+        so_far += w[e];
+        if (!done && so_far >= reach) {
+          finish(at + e, logprob_of(run.element(x, e), best, d.temperature, total), count);
+          done = true;
+        }
+      }
+    }
+    if (before >= reach) break;
   }
 }
 
