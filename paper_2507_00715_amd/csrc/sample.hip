@@ -9,16 +9,17 @@
 // Weights are 64-bit integers, w 2^kFraction rounded: sums of integers do not depend on their order, so the workgroup may add
 // them as it likes (histograms by atomics, prefix sums in any tree) and every call gives the same token.
 //
-// One workgroup a row.  A wave has a run of the row, 16 bytes a lane and unit, and the row stays in registers (UNITS units; 0:
-// any number, read again in every pass).  What bounds a row is how often every entry is touched, by one CU's vector ALU and
-// LDS, so the passes over all entries are few and short:
+// One workgroup a row.  A wave has a run of the row, 16 bytes a lane and unit, which every pass reads again from the caches, four
+// units at a time (held in registers, with the passes unrolled over them, a row of 32000 took as long: the code, 120 KB, came from
+// memory instead).  What bounds a row is how many vector instructions its entries take on their one CU, so the passes over all
+// entries are few and short:
 //   - the largest logit;
 //   - top-k up to kSmallK: a histogram over (l_max - l) / T of the largest entry of every 16 bytes gives a border that at least k
 //     entries reach, and few more: those are listed, and the rest happens in the list;
 //   - else top-k: a histogram of all entries; top-p: one of their weights; the few entries of the bin in which a beginning ends are
 //     ranked among each other;
-//   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept),
-//     then by unit of the wave that u W falls to, all waves together.
+//   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept;
+//     with top-p in the same pass that lists the bin's), then by unit of the wave that u W falls to, all waves together.
 #include <type_traits>
 
 #include "common.h"
@@ -53,6 +54,8 @@ struct SampleSmem {
   int count[kBins];
   u64 list_w[kListMax];
   u64 list_key[kListMax];        // (order key, ~index): larger is earlier in the order
+  u64 sorted[kSmallK];
+  int by_index[kSmallK];
   double power[kExpSteps];       // 2^(i / kExpSteps)
   float queue[WAVES][2 * kWave];
   u64 wave_mass[WAVES];
@@ -61,7 +64,8 @@ struct SampleSmem {
   int wave_at[WAVES];
   int n_list, bin, found_index, before_count;
   float found_value;
-  u64 before_mass, found_mass;
+  u64 before_mass, kept_mass[WAVES];
+  int kept_count[WAVES];
 };
 
 template <typename X>
@@ -87,8 +91,10 @@ struct Weights {
   float bins;         // bins per unit of logit
   double scale;       // 128 log2(e) / T
   const double* power;
-  __device__ __forceinline__ double real(float l) const {
-    const double t = fmax(((double)l - (double)best) * scale, -1100.0 * kExpSteps);
+  __device__ __forceinline__ double real(float l) const { return power_of(fmax(((double)l - (double)best) * scale, -1100.0 * kExpSteps)); }
+  // of an entry that is not in the last bin
+  __device__ __forceinline__ u64 of_near(float l) const { return whole(power_of(((double)l - (double)best) * scale)); }
+  __device__ __forceinline__ double power_of(double t) const {   // 2^(t / kExpSteps)
     const double shifted = t + 0x1.8p52, r = t - (shifted - 0x1.8p52);
     const int n = (int)(unsigned)__double_as_longlong(shifted);
     constexpr double c = 0.69314718055994530942 / kExpSteps;
@@ -107,21 +113,21 @@ struct Weights {
 typedef unsigned int u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned int u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
 
-// The wave's run of the row: unit i, element e of lane is entry begin + (64 i + lane) E + e; -inf past the end and for NaN.
-template <typename T, int UNITS, int WAVES>
+// The wave's run of the row: unit i, element e of lane is entry begin + (64 i + lane) E + e; -inf past the end.
+// (NaN fails every comparison below and falls into the last bin, where it is taken for none of the entries looked for.)
+template <typename T, int WAVES>
 struct Run {
   static constexpr int E = 16 / sizeof(T);
   const T* row;
   int vocab, units, begin, n_units, lane;   // units: of a wave's run, of the last ones fewer
-  bool infinite;                 // the best is +inf: those entries count as 0, all others as -inf
-  u32x4 held[UNITS > 0 ? UNITS : 1];
   __device__ __forceinline__ u32x4 load(int i) const { return load_at(index(i, 0)); }
+  __device__ __forceinline__ u32x4 load_whole(int at) const {
+    if constexpr (sizeof(T) == 4) return *(const u32x4_at4*)((const char*)row + (unsigned)at * 4u);
+    else return *(const u32x4_at2*)((const char*)row + (unsigned)at * 2u);
+  }
   __device__ __forceinline__ u32x4 load_at(int at) const {
     u32x4 x;
-    if (at + E <= vocab) {
-      if constexpr (sizeof(T) == 4) x = *(const u32x4_at4*)(row + at);
-      else x = *(const u32x4_at2*)(row + at);
-    }
+    if (at + E <= vocab) x = load_whole(at);
     else {
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -136,38 +142,31 @@ struct Run {
     return x;
   }
   __device__ __forceinline__ void init(const T* row_, int vocab_, int wave, int lane_) {
-    row = row_; vocab = vocab_; lane = lane_; infinite = false;
+    row = row_; vocab = vocab_; lane = lane_;
     units = ((vocab + WAVES - 1) / WAVES + kWave * E - 1) / (kWave * E);
     begin = min(vocab, wave * units * (kWave * E));
     n_units = min(units, (vocab - begin + kWave * E - 1) / (kWave * E));
-    if constexpr (UNITS > 0) {
-#pragma unroll
-      for (int i = 0; i < UNITS; ++i)
-        if (i < n_units) held[i] = load(i);
-    }
   }
-  __device__ __forceinline__ float element(const u32x4& x, int e) const {
-    float l;
-    if constexpr (sizeof(T) == 4) l = __uint_as_float(x[e]);
-    else l = e & 1 ? bf16_hi(x[e / 2]) : bf16_lo(x[e / 2]);
-    if (infinite) return l == INFINITY ? 0.f : -INFINITY;
-    return fmaxf(l, -INFINITY);
+  __device__ __forceinline__ static float element(const u32x4& x, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(x[e]);
+    else return e & 1 ? bf16_hi(x[e / 2]) : bf16_lo(x[e / 2]);
   }
   __device__ __forceinline__ int index(int i, int e) const { return begin + (kWave * i + lane) * E + e; }
   template <typename F>
   __device__ __forceinline__ void each_unit(F f) const {  // f(first entry, unit)
-    if constexpr (UNITS > 0) {
+    constexpr int TOGETHER = 4;
+    int i = 0;
+#pragma unroll 1
+    for (; i + TOGETHER <= n_units && begin + kWave * E * (i + TOGETHER) <= vocab; i += TOGETHER) {   // whole units
+      const int at = index(i, 0);
+      u32x4 x[TOGETHER];
 #pragma unroll
-      for (int i = 0; i < UNITS; ++i)
-        if (i < n_units) {
-          u32x4 x = held[i];
-          int at = index(i, 0);
-          asm volatile("" : "+v"(x), "+v"(at));   // opaque: what one pass works out of them is not kept, in registers that there are not, for the next
-          f(at, x);
-        }
-    } else {
-      for (int i = 0; i < n_units; ++i) f(index(i, 0), load(i));
+      for (int k = 0; k < TOGETHER; ++k) x[k] = load_whole(at + kWave * E * k);
+#pragma unroll
+      for (int k = 0; k < TOGETHER; ++k) f(at + kWave * E * k, x[k]);
     }
+#pragma unroll 1
+    for (; i < n_units; ++i) f(index(i, 0), load(i));
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {       // f(entry, logit)
@@ -178,11 +177,10 @@ struct Run {
   }
 };
 
-// A beginning of the order: what comes before the logit `value`, and its equals up to entry `index`; they weigh `mass`.
+// A beginning of the order: what comes before the logit `value`, and its equals up to entry `index`.
 struct Beginning {
   float value;
   int index;
-  u64 mass;
   __device__ __forceinline__ bool has(int i, float l) const { return l > value || (l == value && i <= index); }
 };
 
@@ -219,48 +217,42 @@ __device__ __forceinline__ int find_bin(SampleSmem<WAVES>& sm, int k, u64 mass) 
   return sm.bin;
 }
 
-// The beginning that the k-th entry ends, or the first entry at which the weights reach `mass`, of those in `within`; the histogram
-// of these entries is in sm.  There is such an entry.  (The mass of a beginning by count is left to the caller.)  Called by all threads.
-template <bool BY_MASS, typename R, int WAVES>
-__device__ __forceinline__ Beginning find_beginning(const R& run, const Weights& wt, const Beginning& within, int k, u64 mass, SampleSmem<WAVES>& sm) {
-  constexpr int THREADS = kWave * WAVES;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int bin = find_bin<BY_MASS>(sm, k, mass);
-  const int before = BY_MASS ? 0 : sm.before_count;
-  const u64 mass_before = BY_MASS ? sm.before_mass : 0;
-  run.each([&](int i, float l) {
-    if (l > -INFINITY && wt.bin(l) == bin && within.has(i, l)) {
-      const int at = atomicAdd(&sm.n_list, 1);
-      if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
-    }
-  });
+// The index of the r-th entry (1, 2, ...) that equals `value`, in sm.found_index; there is one.  Called by all threads.
+template <typename R, int WAVES>
+__device__ __forceinline__ void find_equal(const R& run, float value, int r, SampleSmem<WAVES>& sm) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int mine = 0;
+  run.each([&](int, float l) { mine += l == value ? 1 : 0; });
+  mine = wave_sum(mine);
   __syncthreads();
-  const int n = sm.n_list;
-  if (n <= kListMax) {
-    if constexpr (BY_MASS) {
-      for (int a = tid; a < n; a += THREADS) sm.list_w[a] = wt.of(key_value((unsigned)(sm.list_key[a] >> 32)));
-      __syncthreads();
+  if (lane == 0) sm.wave_count[wave] = mine;
+  __syncthreads();
+  int at = 0;
+  for (int i = 0; i < wave; ++i) at += sm.wave_count[i];
+  if (at < r && at + mine >= r) {                 // the wave that holds it
+    for (int i = 0; i < run.n_units; ++i) {
+      const u32x4 x = run.load(i);
+      int here = 0;
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) here += run.element(x, e) == value ? 1 : 0;
+      const int upto = at + wave_scan(here, lane);
+      int own = upto - here;
+#pragma unroll
+      for (int e = 0; e < R::E; ++e)
+        if (run.element(x, e) == value && ++own == r) sm.found_index = run.index(i, e);
+      at = __shfl(upto, kWave - 1, kWave);
     }
-    for (int a = tid; a < n; a += THREADS) {
-      const u64 key = sm.list_key[a];
-      int rank = before;
-      u64 weighed = mass_before;
-      for (int b = 0; b < n; ++b) {
-        const bool first = sm.list_key[b] > key;
-        if constexpr (BY_MASS) weighed += first ? sm.list_w[b] : 0;
-        else rank += first ? 1 : 0;
-      }
-      const u64 own = BY_MASS ? sm.list_w[a] : 0;
-      if (BY_MASS ? weighed < mass && weighed + own >= mass : rank == k - 1) {
-        sm.found_value = key_value((unsigned)(key >> 32));
-        sm.found_index = (int)~(unsigned)key;
-        sm.found_mass = weighed + own;
-      }
-    }
-    __syncthreads();
-    return Beginning{sm.found_value, sm.found_index, sm.found_mass};
   }
-  // Too many for the list (mostly equal logits): the last key, bit by bit, then its equals in order of their index.
+  __syncthreads();
+}
+
+// The beginning that the k-th entry ends, or the first entry at which the weights reach `mass`, of those in `within`, where the bin that
+// it ends in holds too many for the list (mostly equal logits): the last key, bit by bit, then its equals in order of their index.
+// Called by all threads.
+template <bool BY_MASS, typename R, int WAVES>
+__device__ __forceinline__ Beginning find_bit_by_bit(const R& run, const Weights& wt, const Beginning& within, int bin, int before, u64 mass_before, int k,
+                                                    u64 mass, SampleSmem<WAVES>& sm) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   auto reach = [&](unsigned key, int& cnt, u64& sum) {   // entries of the bin whose key is at least `key`
     int c = 0;
     u64 m = 0;
@@ -289,30 +281,8 @@ __device__ __forceinline__ Beginning find_beginning(const R& run, const Weights&
   const u64 each_mass = BY_MASS ? wt.of(value) : 0;
   // the r-th equal one is the last
   const int r = BY_MASS ? (int)((mass - sum + each_mass - 1) / each_mass) : k - cnt;
-  int mine = 0;
-  run.each([&](int, float l) { mine += l == value ? 1 : 0; });
-  mine = wave_sum(mine);
-  __syncthreads();
-  if (lane == 0) sm.wave_count[wave] = mine;
-  __syncthreads();
-  int at = 0;
-  for (int i = 0; i < wave; ++i) at += sm.wave_count[i];
-  if (at < r && at + mine >= r) {                 // the wave that holds it
-    for (int i = 0; i < run.n_units; ++i) {
-      const u32x4 x = run.load(i);
-      int here = 0;
-#pragma unroll
-      for (int e = 0; e < R::E; ++e) here += run.element(x, e) == value ? 1 : 0;
-      const int upto = at + wave_scan(here, lane);
-      int own = upto - here;
-#pragma unroll
-      for (int e = 0; e < R::E; ++e)
-        if (run.element(x, e) == value && ++own == r) sm.found_index = run.index(i, e);
-      at = __shfl(upto, kWave - 1, kWave);
-    }
-  }
-  __syncthreads();
-  return Beginning{value, sm.found_index, sum + (u64)r * each_mass};
+  find_equal(run, value, r, sm);
+  return Beginning{value, sm.found_index};
 }
 
 // Sum over the workgroup, in every thread.
@@ -337,75 +307,99 @@ __device__ __forceinline__ float logprob_of(float l, float best, double temperat
   return (float)(z - log((double)total * (1.0 / (double)(1ull << kFraction))));
 }
 
-// Top-k with the rest in the list: its n entries hold the first k.  Four threads an entry share the others.
+// Inclusive prefix sums over the workgroup's threads, on top of `base`; base then is the sum of all.
+template <int WAVES>
+__device__ __forceinline__ u64 block_scan(u64 x, u64& base, SampleSmem<WAVES>& sm) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  x = wave_scan(x, lane);
+  __syncthreads();
+  if (lane == kWave - 1) sm.wave_mass[wave] = x;
+  __syncthreads();
+  x += base;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    const u64 m = sm.wave_mass[i];
+    x += i < wave ? m : 0;
+    base += m;
+  }
+  return x;
+}
+
+// Top-k with the rest in the list: its n entries hold the first k.  They are put in order by counting who comes before whom (four
+// threads an entry), summed up in that order for top-p, then in the order of their indices for the draw.
 template <int WAVES>
 __device__ __forceinline__ void draw_from_list(const SampleParams& p, const Weights& wt, const Draw& d, int n, SampleSmem<WAVES>& sm) {
   constexpr int THREADS = kWave * WAVES;
-  const int tid = threadIdx.x, part = tid % 4, r = blockIdx.x;
-  auto quad = [](auto x) { x += __shfl_xor(x, 1, kWave); return x + __shfl_xor(x, 2, kWave); };
-  for (int a = tid; a < n; a += THREADS) sm.list_w[a] = wt.of(key_value((unsigned)(sm.list_key[a] >> 32)));
-  __syncthreads();
-  constexpr int SLOTS = kListMax * 4 / THREADS;   // entries of a thread: a = tid / 4 + THREADS / 4 * slot
-  int rank[SLOTS];
-  u64 before[SLOTS], first_k = 0;
-#pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    const int a = tid / 4 + THREADS / 4 * s;
-    rank[s] = 0x7fffffff;
-    before[s] = 0;
-    if (THREADS / 4 * s >= n) continue;
+  const int tid = threadIdx.x, part = tid % 4, r = blockIdx.x, k = d.top_k;
+  auto quad = [](int x) { x += __shfl_xor(x, 1, kWave); return x + __shfl_xor(x, 2, kWave); };
+#pragma unroll 1
+  for (int a0 = 0; a0 < n; a0 += THREADS / 4) {
+    const int a = a0 + tid / 4;
     const u64 key = a < n ? sm.list_key[a] : 0;
-    int count = 0;
-    u64 sum = 0;
-    for (int b = part; b < n; b += 4) {
-      const bool first = sm.list_key[b] > key;
-      count += first ? 1 : 0;
-      sum += first ? sm.list_w[b] : 0;
-    }
-    count = quad(count);
-    before[s] = quad(sum);
-    if (a < n) rank[s] = count;
-    if (part == 0 && rank[s] < d.top_k) first_k += sm.list_w[a];
+    int rank = 0;
+#pragma unroll 4
+    for (int b = part; b < n; b += 4) rank += sm.list_key[b] > key ? 1 : 0;
+    rank = quad(rank);
+    if (part == 0 && a < n && rank < k) sm.sorted[rank] = key;
   }
-  first_k = block_sum(first_k, sm);
-  const u64 need = d.top_p < 1.f ? min(max((u64)ceil((double)d.top_p * (double)first_k), (u64)1), first_k) : ~0ull;
-  u64 total = 0;
-  int count = 0;
+  __syncthreads();
+  // in order: what of the first k top-p and min-p keep
+  u64 first_k = 0, total = 0;
+  constexpr int ROUNDS = (kSmallK + THREADS - 1) / THREADS;
+  u64 w[ROUNDS], upto[ROUNDS];
 #pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    const int a = tid / 4 + THREADS / 4 * s;
-    if (a >= n || part != 0) continue;
-    const float l = key_value((unsigned)(sm.list_key[a] >> 32));
-    const bool keep = rank[s] < d.top_k && before[s] < need && wt.real(l) >= d.least;
-    if (!keep) sm.list_w[a] = 0;                  // (an entry of its own: no one else reads it before the next barrier)
-    total += keep ? sm.list_w[a] : 0;
-    count += keep ? 1 : 0;
+  for (int s = 0; s < ROUNDS; ++s) {
+    const int i = s * THREADS + tid;
+    w[s] = i < k ? wt.of(key_value((unsigned)(sm.sorted[i] >> 32))) : 0;
+    upto[s] = s * THREADS < k ? block_scan(w[s], first_k, sm) : 0;
   }
-  total = block_sum(total, sm);
-  count = (int)block_sum((u64)count, sm);
+  const u64 need = d.top_p < 1.f ? min(max((u64)ceil((double)d.top_p * (double)first_k), (u64)1), first_k) : ~0ull;
+  int m = 0;
+#pragma unroll
+  for (int s = 0; s < ROUNDS; ++s) {
+    const int i = s * THREADS + tid;
+    const bool keep = i < k && upto[s] - w[s] < need && wt.real(key_value((unsigned)(sm.sorted[i] >> 32))) >= d.least;
+    m += keep ? 1 : 0;
+    if (i < k) sm.list_w[i] = w[s];
+  }
+  m = (int)block_sum((u64)m, sm);                 // the first m
+  // by index
+#pragma unroll 1
+  for (int a0 = 0; a0 < m; a0 += THREADS / 4) {
+    const int a = a0 + tid / 4;
+    const unsigned index = a < m ? ~(unsigned)sm.sorted[a] : 0;
+    int rank = 0;
+#pragma unroll 4
+    for (int b = part; b < m; b += 4) rank += ~(unsigned)sm.sorted[b] < index ? 1 : 0;
+    rank = quad(rank);
+    if (part == 0 && a < m) sm.by_index[rank] = a;
+  }
+  __syncthreads();
+  int at[ROUNDS];
+#pragma unroll
+  for (int s = 0; s < ROUNDS; ++s) {
+    const int i = s * THREADS + tid;
+    at[s] = i < m ? sm.by_index[i] : 0;
+    w[s] = i < m ? sm.list_w[at[s]] : 0;
+    upto[s] = s * THREADS < m ? block_scan(w[s], total, sm) : 0;
+  }
   const u64 reach = reach_of(d.u, total);
 #pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    const int a = tid / 4 + THREADS / 4 * s;
-    if (THREADS / 4 * s >= n) continue;
-    const u64 key = a < n ? sm.list_key[a] : 0;
-    u64 sum = 0;
-    for (int b = part; b < n; b += 4) sum += (unsigned)sm.list_key[b] > (unsigned)key ? sm.list_w[b] : 0;   // lower indices
-    sum = quad(sum);
-    if (a < n && part == 0 && sum < reach && sum + sm.list_w[a] >= reach) {
-      p.token[r] = (int)~(unsigned)key;
-      if (p.logprob) p.logprob[r] = logprob_of(key_value((unsigned)(key >> 32)), wt.best, d.temperature, total);
-      if (p.n_kept) p.n_kept[r] = count;
-    }
+  for (int s = 0; s < ROUNDS; ++s) {
+    if (s * THREADS + tid >= m || !(upto[s] - w[s] < reach && upto[s] >= reach)) continue;
+    const u64 key = sm.sorted[at[s]];
+    p.token[r] = (int)~(unsigned)key;
+    if (p.logprob) p.logprob[r] = logprob_of(key_value((unsigned)(key >> 32)), wt.best, d.temperature, total);
+    if (p.n_kept) p.n_kept[r] = m;
   }
 }
 
-template <typename T, int UNITS, int WAVES>
+template <typename T, int WAVES>
 __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   constexpr int THREADS = kWave * WAVES;
   __shared__ SampleSmem<WAVES> sm;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), r = blockIdx.x;
-  Run<T, UNITS, WAVES> run;
+  Run<T, WAVES> run;
   run.init((const T*)p.logits + (long long)r * p.row_stride, p.vocab, wave, lane);
   const float temperature = p.temperature ? p.temperature[r] : 1.f;
   const int top_k = p.top_k ? p.top_k[r] : 0;
@@ -415,7 +409,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   for (int i = tid; i < kExpSteps; i += THREADS) sm.power[i] = exp2((double)i / kExpSteps);
   for (int i = tid; i < kBins; i += THREADS) { sm.mass[i] = 0; sm.count[i] = 0; }
   float best = -INFINITY;
-  run.each([&](int, float l) { best = fmaxf(best, l); });
+  run.each([&](int, float l) { best = l > best ? l : best; });
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) best = fmaxf(best, __shfl_xor(best, o, kWave));
   if (lane == 0) sm.wave_best[wave] = best;
@@ -441,7 +435,16 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
     }
     return;
   }
-  if (best == INFINITY) { run.infinite = true; best = 0.f; }
+  if (best == INFINITY) {                         // the infinite ones alone, at equal weights: the first of them by index
+    int n = 0;
+    run.each([&](int, float l) { n += l == INFINITY ? 1 : 0; });
+    u64 m = block_sum((u64)n, sm);
+    if (top_k > 0 && (u64)top_k < m) m = (u64)top_k;
+    if (top_p < 1.f) m = min(max((u64)ceil((double)top_p * (double)m), (u64)1), m);
+    find_equal(run, INFINITY, (int)reach_of((double)u, m), sm);
+    if (tid == 0) finish(sm.found_index, (float)-log((double)m), (int)m);
+    return;
+  }
 
   Weights wt;
   wt.best = best;
@@ -449,25 +452,24 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   wt.bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
   wt.power = sm.power;
   const Draw d{(double)u, (double)temperature, top_p, min_p > 0.f ? (double)fminf(min_p, 1.f) : 0.0, top_k};
-  typedef Run<T, UNITS, WAVES> R;
-  Beginning kept{-INFINITY, -1, 0};
+  typedef Run<T, WAVES> R;
+  Beginning kept{-INFINITY, -1};
+  auto list_key = [&](int i, float l) {
+    const int at = atomicAdd(&sm.n_list, 1);
+    if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
+  };
   bool limited = false;
   if (top_k > 0) {
     if (top_k <= kSmallK) {
       run.each_unit([&](int, const u32x4& x) {
         float most = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < R::E; ++e) most = fmaxf(most, run.element(x, e));
+        for (int e = 0; e < R::E; ++e) { const float l = run.element(x, e); most = l > most ? l : most; }
         if (most > -INFINITY) atomicAdd(&sm.count[wt.bin(most)], 1);
       });
       const int bin = find_bin<false>(sm, top_k, 0);
       if (bin < kBins - 1) {
-        run.each([&](int i, float l) {
-          if (wt.bin(l) <= bin) {
-            const int at = atomicAdd(&sm.n_list, 1);
-            if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
-          }
-        });
+        run.each([&](int i, float l) { if (wt.bin(l) <= bin) list_key(i, l); });
         __syncthreads();
         const int n = sm.n_list;
         if (n <= kListMax) { draw_from_list(p, wt, d, n, sm); return; }
@@ -482,56 +484,114 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
       if (l > -INFINITY) { atomicAdd(&sm.count[wt.bin(l)], 1); ++n_finite; }
     });
     limited = block_sum((u64)n_finite, sm) > (u64)top_k;
-    if (limited) kept = find_beginning<false, R, WAVES>(run, wt, kept, top_k, 0, sm);
+    if (limited) {
+      const int bin = find_bin<false>(sm, top_k, 0), before = sm.before_count;
+      run.each([&](int i, float l) { if (l > -INFINITY && wt.bin(l) == bin) list_key(i, l); });
+      __syncthreads();
+      const int n = sm.n_list;
+      if (n <= kListMax) {
+        for (int a = tid; a < n; a += THREADS) {
+          const u64 key = sm.list_key[a];
+          int rank = before;
+          for (int b = 0; b < n; ++b) rank += sm.list_key[b] > key ? 1 : 0;
+          if (rank == top_k - 1) { sm.found_value = key_value((unsigned)(key >> 32)); sm.found_index = (int)~(unsigned)key; }
+        }
+        __syncthreads();
+        kept = Beginning{sm.found_value, sm.found_index};
+      } else kept = find_bit_by_bit<false>(run, wt, kept, bin, before, 0, top_k, 0, sm);
+    }
   }
-  if (top_p < 1.f) {
-    u64 all = 0;
-    run.each([&](int i, float l) {
-      const int b = wt.bin(l);
-      if (b < kBins - 1 && kept.has(i, l)) {
-        const u64 w = wt.of(l);
-        atomicAdd(&sm.mass[b], w);
-        all += w;
-      }
-    });
-    all = block_sum(all, sm);
-    kept = find_beginning<true, R, WAVES>(run, wt, kept, 0, min(max((u64)ceil((double)top_p * (double)all), (u64)1), all), sm);
-    limited = true;
-  }
+  // the kept weights of each wave's run
   auto weight = [&](float l, bool& in) {          // of an entry of the beginning
     const double x = wt.real(l);
     in = x >= d.least;
     return in ? Weights::whole(x) : (u64)0;
   };
-  // the kept weights of each wave's run
   u64 mine = 0;
-  int count = 0;
-  if (limited) {                                  // few entries, as a rule: gathered before their weights are worked out
-    float* queue = sm.queue[wave];
-    int waiting = 0;
-    auto take = [&](int n) {                      // the first n <= 64 of the queue
-      bool in;
-      const u64 w = weight(queue[lane], in);
-      if (lane < n) { mine += w; count += in ? 1 : 0; }
+  int count = 0, waiting = 0;
+  float* queue = sm.queue[wave];
+  auto take = [&](int n) {                        // the first n <= 64 of the queue
+    bool in;
+    const u64 w = weight(queue[lane], in);
+    if (lane < n) { mine += w; count += in ? 1 : 0; }
+  };
+  // few entries of many, as a rule: gathered before their weights are worked out
+  auto gather = [&](bool has, float l) {
+    const unsigned long long who = __ballot(has);
+    if (who == 0) return;
+    if (has) queue[waiting + __popcll(who & ((1ull << lane) - 1))] = l;
+    asm volatile("" ::: "memory");                // the wave's LDS operations complete in order: only the compiler has to keep theirs
+    waiting += __popcll(who);
+    if (waiting >= kWave) {
+      take(kWave);
+      const float rest = queue[kWave + lane];
+      asm volatile("" ::: "memory");
+      queue[lane] = rest;
+      asm volatile("" ::: "memory");
+      waiting -= kWave;
+    }
+  };
+  bool summed = false;
+  if (top_p < 1.f) {
+    u64 all = 0;
+    auto add_mass = [&](float l, int b) {
+      const u64 w = wt.of_near(l);
+      atomicAdd(&sm.mass[b], w);
+      all += w;
     };
-    run.each([&](int i, float l) {
-      const bool has = kept.has(i, l);
-      const unsigned long long who = __ballot(has);
-      if (who == 0) return;
-      if (has) queue[waiting + __popcll(who & ((1ull << lane) - 1))] = l;
-      asm volatile("" ::: "memory");              // the wave's LDS operations complete in order: only the compiler has to keep theirs
-      waiting += __popcll(who);
-      if (waiting >= kWave) {
-        take(kWave);
-        const float rest = queue[kWave + lane];
-        asm volatile("" ::: "memory");
-        queue[lane] = rest;
-        asm volatile("" ::: "memory");
-        waiting -= kWave;
-      }
+    if (limited) run.each([&](int i, float l) {
+      const int b = wt.bin(l);
+      if (b < kBins - 1 && kept.has(i, l)) add_mass(l, b);
     });
+    else run.each([&](int, float l) {
+      const int b = wt.bin(l);
+      if (b < kBins - 1) add_mass(l, b);
+    });
+    all = block_sum(all, sm);
+    const u64 need = min(max((u64)ceil((double)top_p * (double)all), (u64)1), all);
+    const int bin = find_bin<true>(sm, 0, need);
+    const u64 before = sm.before_mass;
+    if (tid < WAVES) { sm.kept_mass[tid] = 0; sm.kept_count[tid] = 0; }
+    run.each([&](int i, float l) {
+      const int b = wt.bin(l);
+      const bool in = !limited || kept.has(i, l);
+      if (in && b == bin) list_key(i, l);
+      gather(in && b < bin, l);
+    });
+    __syncthreads();
+    const int n = sm.n_list;
+    if (n <= kListMax) {
+      summed = true;
+      for (int a = tid; a < n; a += THREADS) sm.list_w[a] = wt.of(key_value((unsigned)(sm.list_key[a] >> 32)));
+      __syncthreads();
+      for (int a = tid; a < n; a += THREADS) {
+        const u64 key = sm.list_key[a], own = sm.list_w[a];
+        u64 weighed = before;
+        for (int b = 0; b < n; ++b) weighed += sm.list_key[b] > key ? sm.list_w[b] : 0;
+        if (weighed >= need) continue;            // behind the beginning
+        const float l = key_value((unsigned)(key >> 32));
+        const int i = (int)~(unsigned)key, holder = i / (run.units * (kWave * R::E));
+        bool in;
+        const u64 w = weight(l, in);
+        if (in) { atomicAdd(&sm.kept_mass[holder], w); atomicAdd(&sm.kept_count[holder], 1); }
+        if (weighed + own >= need) { sm.found_value = l; sm.found_index = i; }
+      }
+      __syncthreads();
+      kept = Beginning{sm.found_value, sm.found_index};
+      if (waiting > 0) take(waiting);
+      mine += lane == 0 ? sm.kept_mass[wave] : 0;
+      count += lane == 0 ? sm.kept_count[wave] : 0;
+    } else {
+      kept = find_bit_by_bit<true>(run, wt, kept, bin, 0, before, 0, need, sm);
+      mine = 0;
+      count = waiting = 0;
+    }
+    limited = true;
+  }
+  if (!summed && limited) {
+    run.each([&](int i, float l) { gather(kept.has(i, l), l); });
     if (waiting > 0) take(waiting);
-  } else {
+  } else if (!summed) {
     run.each([&](int, float l) {
       if (l > -INFINITY) {
         bool in;
@@ -594,11 +654,8 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
 
 template <typename T>
 static void launch_sample_t(const SampleParams& p, int rows, hipStream_t stream) {
-  constexpr int E = 16 / sizeof(T), small = 4 * 4 * kWave * E, middle = 16 * 8 * kWave * E, large = 16 * 16 * kWave * E;
-  if (p.vocab <= small) hipLaunchKernelGGL((sample_kernel<T, 4, 4>), dim3(rows), dim3(4 * kWave), 0, stream, p);
-  else if (p.vocab <= middle) hipLaunchKernelGGL((sample_kernel<T, 8, 16>), dim3(rows), dim3(16 * kWave), 0, stream, p);
-  else if (p.vocab <= large) hipLaunchKernelGGL((sample_kernel<T, 16, 16>), dim3(rows), dim3(16 * kWave), 0, stream, p);
-  else hipLaunchKernelGGL((sample_kernel<T, 0, 16>), dim3(rows), dim3(16 * kWave), 0, stream, p);
+  if (p.vocab <= 4 * 4 * kWave * 16 / (int)sizeof(T)) hipLaunchKernelGGL((sample_kernel<T, 4>), dim3(rows), dim3(4 * kWave), 0, stream, p);
+  else hipLaunchKernelGGL((sample_kernel<T, 16>), dim3(rows), dim3(16 * kWave), 0, stream, p);
 }
 
 int launch_sample(const void* logits, int dtype, int64_t row_stride, int rows, int vocab, const float* temperature,
