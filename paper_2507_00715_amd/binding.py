@@ -459,71 +459,102 @@ def earn_cache_entries(n_layers: int, split_k: int, seq_len: int, n_registers: i
     return int(lib().earn_cache_entries(n_layers, split_k, seq_len, n_registers, gen))
 
 
-def _ws(workspace, need: int, device):
-    """A workspace and its size: the caller's, or one for this call (loops pass a buffer of their own)."""
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, (0 if workspace is None else workspace.numel() * workspace.element_size())
+def _on(dev: int, *tensors):
+    """Addresses of contiguous tensors on device `dev`, the current one: a call goes to a stream of that device."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != dev or not t.is_contiguous():
+            raise AssertionError("libearn takes contiguous tensors of the current device")
+        out.append(t.data_ptr())
+    return out
 
 
-def _typed(dtype: torch.dtype, **tensors) -> None:
-    """The library is told no element types of index and weight arrays: they have to be what the header says."""
-    for name, t in tensors.items():
-        assert t is None or t.dtype == dtype, f"{name} must be {dtype}"
+def _size(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _current() -> int:
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    return torch._C._cuda_getDevice()
 
 
 def _pool(k_pages, v_pages, desc: AttnDesc):
     """(n_pages, page_size) of [n_pages, Hkv, page_size, d] pools."""
-    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape, "k_pages, v_pages: [n_pages, Hkv, page_size, d]"
-    assert k_pages.shape[1] == desc.n_kv_heads and k_pages.shape[3] == desc.head_dim, "the pools have other heads than the description"
-    assert k_pages.element_size() == v_pages.element_size() == (4 if desc.dtype == EARN_F32 else 2), "the pools have another type than the description"
-    return k_pages.shape[0], k_pages.shape[2]
+    n_pages, heads, page_size, d = k_pages.shape
+    assert heads == desc.n_kv_heads and d == desc.head_dim, "the pools [n_pages, Hkv, page_size, d] have other heads than the description"
+    assert v_pages.shape == k_pages.shape and v_pages.dtype is k_pages.dtype
+    assert k_pages.dtype is (torch.float32 if desc.dtype == EARN_F32 else torch.bfloat16), "the pools have another type than the description"
+    return n_pages, page_size
+
+
+def _i32(*tensors) -> None:
+    """The library is told no types of index arrays: they have to be what the header says."""
+    for t in tensors:
+        assert t is None or t.dtype is torch.int32, "index arrays are int32"
+
+
+def _f32(*tensors) -> None:
+    for t in tensors:
+        assert t is None or t.dtype is torch.float32, "weights and parameters are fp32"
 
 
 def earn_cache_store(desc: AttnDesc, k, v, cu_seqlens, start, k_pages, v_pages, page_table) -> None:
     """Rows of a prefill to their pages; cu_seqlens [batch + 1], start [batch] or None, page_table [batch, max_pages]."""
     n_pages, page_size = _pool(k_pages, v_pages, desc)
-    _typed(torch.int32, cu_seqlens=cu_seqlens, start=start, page_table=page_table)
-    batch = page_table.shape[0]
-    assert cu_seqlens.numel() == batch + 1 and (start is None or start.numel() == batch) and k.shape == v.shape
-    assert tuple(k.shape[1:]) == (desc.n_kv_heads, desc.head_dim) and k.dtype == v.dtype == k_pages.dtype
-    _check(lib().earn_cache_store(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(start), batch, _rows(k),
-                                  _ptr(k_pages), _ptr(v_pages), _ptr(page_table), page_table.shape[1], n_pages, page_size,
-                                  _stream()))
+    _i32(cu_seqlens, start, page_table)
+    batch, max_pages = page_table.shape
+    total, heads, d = k.shape
+    assert heads == desc.n_kv_heads and d == desc.head_dim and v.shape == k.shape and k.dtype is v.dtype is k_pages.dtype
+    assert cu_seqlens.numel() == batch + 1 and (start is None or start.numel() == batch)
+    a = _on(_current(), k, v, cu_seqlens, start, k_pages, v_pages, page_table)
+    _check(lib().earn_cache_store(ctypes.byref(desc), a[0], a[1], a[2], a[3], batch, total, a[4], a[5], a[6], max_pages, n_pages,
+                                  page_size, _stream()))
 
 
 def earn_decode_paged_workspace_bytes(desc: AttnDesc, n_streams: int, max_cache_len: int, have_weights: bool) -> int:
     return int(lib().earn_decode_paged_workspace_bytes(ctypes.byref(desc), n_streams, max_cache_len, int(bool(have_weights))))
 
 
+def _decode_paged_args(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len: int, out,
+                       weights_in, weights_out, workspace):
+    n_pages, page_size = _pool(k_pages, v_pages, desc)
+    _i32(q_pos, page_table, cache_len)
+    n, max_pages = page_table.shape
+    hkv, d = desc.n_kv_heads, desc.head_dim
+    assert q.shape == out.shape == (n, desc.n_q_heads, d) and k_new.shape == v_new.shape == (n, hkv, d)
+    assert q.dtype is k_new.dtype is v_new.dtype is out.dtype is k_pages.dtype
+    assert q_pos.numel() == cache_len.numel() == n
+    rows = 0
+    if weights_out is not None:
+        _f32(weights_in, weights_out)
+        rows = weights_out.shape[-1]
+        assert weights_out.shape == (n, hkv, rows) and (weights_in is None or weights_in.shape == weights_out.shape)
+    if workspace is None:   # one-off calls; loops pass a buffer of their own
+        need = earn_decode_paged_workspace_bytes(desc, n, max_cache_len, weights_out is not None)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    a = _on(_current(), q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, weights_in, weights_out, out, workspace)
+    return (ctypes.byref(desc), *a[:8], n, max_pages, n_pages, page_size, max_cache_len, a[8], a[9], rows, a[10], a[11],
+            _size(workspace)), workspace
+
+
 def bind_decode_attn_paged(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len: int,
                            out, weights_in=None, weights_out=None, workspace=None) -> BoundCall:
     """earn_decode_attn_paged with the same arguments, marshalled once (see BoundCall)."""
-    n_pages, page_size = _pool(k_pages, v_pages, desc)
-    n = page_table.shape[0]
-    _typed(torch.int32, q_pos=q_pos, page_table=page_table, cache_len=cache_len)
-    _typed(torch.float32, weights_in=weights_in, weights_out=weights_out)
-    _typed(k_pages.dtype, q=q, k_new=k_new, v_new=v_new, out=out)
-    assert q_pos.numel() == cache_len.numel() == n and q.shape == out.shape == (n, desc.n_q_heads, desc.head_dim)
-    assert k_new.shape == v_new.shape == (n, desc.n_kv_heads, desc.head_dim)
-    rows = 0
-    if weights_out is not None:
-        rows = weights_out.shape[-1]
-        assert tuple(weights_out.shape) == (n, desc.n_kv_heads, rows)
-        assert weights_in is None or weights_in.shape == weights_out.shape
-    workspace, ws_bytes = _ws(workspace, earn_decode_paged_workspace_bytes(desc, n, max_cache_len, weights_out is not None)
-                              if workspace is None else 0, q.device)
-    args = (ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_pos), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-            _ptr(cache_len), n, page_table.shape[1], n_pages, page_size, max_cache_len, _ptr(weights_in), _ptr(weights_out), rows,
-            _ptr(out), _ptr(workspace), ws_bytes)
+    args, workspace = _decode_paged_args(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len, out,
+                                         weights_in, weights_out, workspace)
     return BoundCall(lib().earn_decode_attn_paged, args, (desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len,
                                                           weights_in, weights_out, out, workspace))
 
 
 def earn_decode_attn_paged(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len: int,
                            out, weights_in=None, weights_out=None, workspace=None) -> None:
-    bind_decode_attn_paged(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len, out, weights_in,
-                           weights_out, workspace)()
+    args, workspace = _decode_paged_args(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, max_cache_len, out,
+                                         weights_in, weights_out, workspace)
+    _check(lib().earn_decode_attn_paged(*args, _stream()))
 
 
 def earn_cache_evict_workspace_bytes(desc: AttnDesc, n_streams: int, max_cache_len: int, budget: int) -> int:
@@ -533,19 +564,19 @@ def earn_cache_evict_workspace_bytes(desc: AttnDesc, n_streams: int, max_cache_l
 def earn_cache_evict(desc: AttnDesc, k_pages, v_pages, page_table, cache_len, max_cache_len: int, weights, budget: int,
                      n_first: int, n_last: int, new_table, kept_out, len_out, weights_out=None, workspace=None) -> None:
     n_pages, page_size = _pool(k_pages, v_pages, desc)
-    n, hkv = page_table.shape[0], desc.n_kv_heads
-    _typed(torch.int32, page_table=page_table, cache_len=cache_len, new_table=new_table, kept_out=kept_out, len_out=len_out)
-    _typed(torch.float32, weights=weights, weights_out=weights_out)
-    assert cache_len.numel() == len_out.numel() == n and new_table.shape[0] == n
-    assert tuple(weights.shape[:2]) == (n, hkv) and tuple(kept_out.shape) == (n, hkv, budget)
-    assert weights_out is None or tuple(weights_out.shape[:2]) == (n, hkv)
-    workspace, ws_bytes = _ws(workspace, earn_cache_evict_workspace_bytes(desc, n, max_cache_len, budget) if workspace is None else 0,
-                              k_pages.device)
-    _check(lib().earn_cache_evict(ctypes.byref(desc), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_len), n,
-                                  page_table.shape[1], n_pages, page_size, max_cache_len, _ptr(weights), weights.shape[2], budget,
-                                  n_first, n_last, _ptr(new_table), new_table.shape[1], _ptr(kept_out), _ptr(len_out),
-                                  _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2], _ptr(workspace), ws_bytes,
-                                  _stream()))
+    n, max_pages = page_table.shape
+    hkv = desc.n_kv_heads
+    _i32(page_table, cache_len, new_table, kept_out, len_out)
+    _f32(weights, weights_out)
+    assert cache_len.numel() == len_out.numel() == n and new_table.shape[0] == n and kept_out.shape == (n, hkv, budget)
+    assert weights.shape[:2] == (n, hkv) and (weights_out is None or weights_out.shape[:2] == (n, hkv))
+    if workspace is None:
+        need = earn_cache_evict_workspace_bytes(desc, n, max_cache_len, budget)
+        workspace = torch.empty(need, dtype=torch.uint8, device=k_pages.device) if need else None
+    a = _on(_current(), k_pages, v_pages, page_table, cache_len, weights, new_table, kept_out, len_out, weights_out, workspace)
+    _check(lib().earn_cache_evict(ctypes.byref(desc), *a[:4], n, max_pages, n_pages, page_size, max_cache_len, a[4], weights.shape[2],
+                                  budget, n_first, n_last, a[5], new_table.shape[1], a[6], a[7], a[8],
+                                  0 if weights_out is None else weights_out.shape[2], a[9], _size(workspace), _stream()))
 
 
 def earn_sample_workspace_bytes(rows: int, vocab: int) -> int:
@@ -555,14 +586,17 @@ def earn_sample_workspace_bytes(rows: int, vocab: int) -> int:
 def earn_sample(logits, uniform, token_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob_out=None,
                 n_kept_out=None, workspace=None) -> None:
     """logits [rows, vocab], fp32 or bf16, rows at any distance (a slice of wider rows is taken as it is)."""
-    code = {torch.float32: EARN_F32, torch.bfloat16: EARN_BF16}.get(logits.dtype, 99)
+    code = EARN_F32 if logits.dtype is torch.float32 else EARN_BF16 if logits.dtype is torch.bfloat16 else 99
     rows, vocab = logits.shape
-    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1), "the logits of a row must lie side by side"
-    _typed(torch.float32, uniform=uniform, temperature=temperature, top_p=top_p, min_p=min_p, logprob_out=logprob_out)
-    _typed(torch.int32, top_k=top_k, token_out=token_out, n_kept_out=n_kept_out)
+    dev = _current()
+    assert logits.get_device() == dev and (vocab <= 1 or logits.stride(1) == 1), "the logits of a row lie side by side on the current device"
+    _f32(uniform, temperature, top_p, min_p, logprob_out)
+    _i32(top_k, token_out, n_kept_out)
     for t in (uniform, token_out, temperature, top_k, top_p, min_p, logprob_out, n_kept_out):
         assert t is None or t.numel() == rows, "one entry a row"
-    workspace, ws_bytes = _ws(workspace, earn_sample_workspace_bytes(rows, vocab) if workspace is None else 0, logits.device)
-    _check(lib().earn_sample(ctypes.c_void_p(logits.data_ptr()), code, logits.stride(0) if rows > 1 else vocab, rows, vocab,
-                             _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(token_out),
-                             _ptr(logprob_out), _ptr(n_kept_out), _ptr(workspace), ws_bytes, _stream()))
+    if workspace is None:
+        need = earn_sample_workspace_bytes(rows, vocab)
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+    a = _on(dev, temperature, top_k, top_p, min_p, uniform, token_out, logprob_out, n_kept_out, workspace)
+    _check(lib().earn_sample(logits.data_ptr(), code, logits.stride(0) if rows > 1 else vocab, rows, vocab, *a, _size(workspace),
+                             _stream()))
