@@ -58,13 +58,15 @@ __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restric
     x[i] = __builtin_nontemporal_load(k + row * UPR + unit);
     y[i] = __builtin_nontemporal_load(v + row * UPR + unit);
   }
+  // the sequence of the workgroup's first token, looked up once; later ones are the same or follow it
+  auto token_of = [&](long long row) { return rows < 0x7fffffff ? (int)by_heads.div((unsigned)row) : (int)(row / pg.hkv); };
+  int s = find_seq(cu, batch, token_of((long long)blockIdx.x * (STEP * kStoreUnits)));
 #pragma unroll
   for (int i = 0; i < kStoreUnits; ++i) {
     const long long row = row0 + i * STEP;
     if (row >= rows) continue;
-    const int token = rows < 0x7fffffff ? (int)by_heads.div((unsigned)row) : (int)(row / pg.hkv);
-    const int c = (int)(row - (long long)token * pg.hkv);
-    const int s = find_seq(cu, batch, token);
+    const int token = token_of(row), c = (int)(row - (long long)token * pg.hkv);
+    while (s + 1 < batch && cu[s + 1] <= token) ++s;
     int b0, n;
     clamped_bounds(cu, s, total, total, b0, n);
     if (token < b0 || token >= b0 + n) continue;   // behind the last sequence
@@ -885,8 +887,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   u32x4 k = {0u, 0u, 0u, 0u}, v = k;             // a row without a page: zeros
   if (old >= 0) {
     const long long from = row_offset<D>(p.pg, old, c, in_old) * (long long)sizeof(T) / 16 + unit;
-    k = ((const u32x4*)p.pg.k)[from];
-    v = ((const u32x4*)p.pg.v)[from];
+    k = __builtin_nontemporal_load((const u32x4*)p.pg.k + from);
+    v = __builtin_nontemporal_load((const u32x4*)p.pg.v + from);
   }
   ((u32x4*)p.pg.k)[to] = k;
   ((u32x4*)p.pg.v)[to] = v;
