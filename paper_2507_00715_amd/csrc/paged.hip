@@ -943,12 +943,18 @@ static int paged_parts(const earn_attn_desc* desc) {
 static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
   PagedPlan pl{};
   const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
+  // Rows of a split: what leaves a workgroup per CU (fp32, whose workgroups are lighter: two), from 256, below
+  // which a workgroup's start costs more than its rows, to 1088, above which the long streams' last splits run on their own.  Up to
+  // 640 rows nothing is split: the joining launch costs as much as it saves.  us, 256 / 512 / 1024 / 2048 rows: 8 streams of 2000 rows, 32
+  // / 32 heads 65 / 61 / 60 / 58; 4 of 8192, 32 / 8 heads 37 / 35 / 29 / 36; one of 4096 14 / 16 / 22 / 34; 16 of 8192-32768 270 / 228 / 214
+  // / 212; one of 65521, 12 / 2 heads 26 / 24 / 27 / 39; one of 32768, fp32 74 / 64 / 70 / 118; 32 of 256-528, 14 / 2 heads of 64 12.2 / 14.4 /
+  // 11.5 whole; 256 of 100-500, 12 / 2 heads 29 / 20 whole.
   const int forced = tuning(kTunePagedChunk, 0);
-  long long chunk = rows * pairs / 4096;
+  long long chunk = rows * pairs / (desc->dtype == EARN_F32 ? 512 : 256);
   if (chunk < 256) chunk = 256;
+  if (chunk > 1088) chunk = 1088;
   if (rows <= 640) chunk = rows;
-  if (forced > 0) chunk = forced;
-  if (chunk > kPagedMaxChunk) chunk = kPagedMaxChunk;
+  if (forced > 0) chunk = forced < kPagedMaxChunk ? forced : kPagedMaxChunk;
   if (chunk > rows) chunk = rows;
   pl.chunk = (int)((chunk + 63) / 64 * 64);
   pl.n_splits = (int)((rows + pl.chunk - 1) / pl.chunk);
