@@ -50,7 +50,7 @@ extern "C" {
 #define EARN_BF16 1
 
 /* Longest cache the calls over pages take. */
-#define EARN_MAX_CACHE_LEN (1 << 30)
+#define EARN_MAX_CACHE_LEN (1 << 26)
 /* Largest number of tensors one earn_compact_registers call gathers. */
 #define EARN_MAX_COMPACT_TENSORS 112
 
@@ -457,6 +457,7 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  *   workspace   at least earn_cache_evict_workspace_bytes(...) bytes; may be NULL when that is 0
  * Errors: NULL required pointer, non-positive size, n_first or n_last < 0, n_first + n_last > budget, a bound that does not hold
  * -> INVALID_ARG; desc as for earn_prefill_attn (dtype, n_kv_heads, head_dim are used).
+ * max_cache_len and budget go up to EARN_MAX_CACHE_LEN, n_streams up to 65535.
  */
 int earn_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* start,
                      int32_t batch, int32_t total_tokens, void* k_pages, void* v_pages, const int32_t* page_table,
@@ -496,7 +497,7 @@ size_t earn_cache_evict_workspace_bytes(const earn_attn_desc* desc, int32_t n_st
  *   n_kept_out   [rows] int32 or NULL: how many tokens were kept
  *   workspace    at least earn_sample_workspace_bytes(rows, vocab) bytes, 256-byte aligned; may be NULL when that is 0
  * All arrays in device memory.  Errors: NULL logits, uniform or token_out, non-positive size, row_stride < vocab -> INVALID_ARG;
- * unknown dtype, vocab > 524288 -> UNSUPPORTED.  rows == 0 is a no-op.
+ * unknown dtype, vocab > 524288, rows > 2^21 -> UNSUPPORTED.  rows == 0 is a no-op.
  */
 int earn_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
                 const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* token_out,

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <exception>
 #include <vector>
 
 #include "common.h"
@@ -244,6 +245,81 @@ static int validate_lengths(const char* who, const std::vector<int32_t>& len, in
   for (size_t u = 0; u < len.size(); ++u)
     if (len[u] > max_len) { set_error("%s: cache_len[%zu] = %d, more than the bound %d passed by value", who, u, len[u], max_len); return EARN_ERR_INVALID_ARG; }
   return EARN_OK;
+}
+
+static int validate_store(const char* who, const int32_t* cu_seqlens, const int32_t* start, const int32_t* page_table, int batch, int total_tokens, int max_pages,
+                          int n_pages, int page_size, void* stream) {
+  int rc;
+  std::vector<int32_t> cu, st((size_t)batch, 0), table;
+  if ((rc = fetch_i32(cu_seqlens, (size_t)batch + 1, cu, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = validate_cu(who, "cu_seqlens", cu, batch, total_tokens, 0x7fffffff)) != EARN_OK) return rc;
+  if (start && (rc = fetch_i32(start, (size_t)batch, st, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = fetch_i32(page_table, (size_t)batch * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  std::vector<long long> rows((size_t)batch), from((size_t)batch), to((size_t)batch);
+  for (int s = 0; s < batch; ++s) {
+    if (st[s] < 0) { set_error("%s: start[%d] = %d is negative", who, s, st[s]); return EARN_ERR_INVALID_ARG; }
+    const int n = cu[s + 1] - cu[s];
+    rows[s] = n > 0 ? (long long)st[s] + n : 0;
+    to[s] = (rows[s] + page_size - 1) / page_size;
+    from[s] = n > 0 ? st[s] / page_size : to[s];
+  }
+  if ((rc = validate_table(who, "page_table", table, batch, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+  std::vector<int32_t> taken((size_t)n_pages, 0);
+  if ((rc = validate_written(who, "page_table", table, batch, max_pages, from, to, taken)) != EARN_OK) return rc;
+  return EARN_OK;
+}
+static int validate_decode_paged(const char* who, const int32_t* q_pos, const int32_t* cache_len, const int32_t* page_table, int n_streams, int max_cache_len,
+                                 int max_pages, int n_pages, int page_size, void* stream) {
+  int rc;
+  std::vector<int32_t> qp, len, table;
+  if ((rc = fetch_i32(q_pos, (size_t)n_streams, qp, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
+  std::vector<long long> rows((size_t)n_streams), from((size_t)n_streams), to((size_t)n_streams);
+  for (int u = 0; u < n_streams; ++u) {
+    if (len[u] < 0) qp[u] = 0;                   // an idle stream's position is not read
+    rows[u] = len[u] < 0 ? 0 : (long long)len[u] + 1;
+    to[u] = (rows[u] + page_size - 1) / page_size;
+    from[u] = rows[u] > 0 ? to[u] - 1 : 0;
+  }
+  if ((rc = validate_positions(who, "q_pos", qp)) != EARN_OK) return rc;
+  if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+  std::vector<int32_t> taken((size_t)n_pages, 0);
+  if ((rc = validate_written(who, "page_table", table, n_streams, max_pages, from, to, taken)) != EARN_OK) return rc;
+  return EARN_OK;
+}
+static int validate_evict(const char* who, const int32_t* cache_len, const int32_t* page_table, const int32_t* new_table, int n_streams, int max_cache_len,
+                          int budget, int max_pages, int new_max_pages, int n_pages, int page_size, void* stream) {
+  int rc;
+  std::vector<int32_t> len, table, fresh;
+  if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
+  if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  if ((rc = fetch_i32(new_table, (size_t)n_streams * new_max_pages, fresh, (hipStream_t)stream, who)) != EARN_OK) return rc;
+  std::vector<long long> rows((size_t)n_streams), kept((size_t)n_streams), zero((size_t)n_streams, 0), to((size_t)n_streams);
+  for (int u = 0; u < n_streams; ++u) {
+    rows[u] = len[u] < 0 ? 0 : len[u];
+    kept[u] = rows[u] < budget ? rows[u] : budget;
+    to[u] = (kept[u] + page_size - 1) / page_size;
+  }
+  if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
+  if ((rc = validate_table(who, "new_table", fresh, n_streams, new_max_pages, n_pages, page_size, kept)) != EARN_OK) return rc;
+  std::vector<int32_t> taken((size_t)n_pages, 0);
+  for (int u = 0; u < n_streams; ++u)
+    for (long long i = 0; i * page_size < rows[u]; ++i) taken[table[(size_t)u * max_pages + i]] = 1;
+  if ((rc = validate_written(who, "new_table", fresh, n_streams, new_max_pages, zero, to, taken)) != EARN_OK) return rc;
+  return EARN_OK;
+}
+// A check in a host memory that may not be enough for the tables: no exception leaves a C entry.
+template <typename F>
+static int guarded(const char* who, F check) {
+  try {
+    return check();
+  } catch (const std::exception&) {
+    set_error("%s: validation ran out of host memory", who);
+    return EARN_ERR_HIP;
+  }
 }
 
 }  // namespace earn
@@ -727,24 +803,7 @@ int earn_cache_store(const earn_attn_desc* desc, const void* k, const void* v, c
   if (total_tokens == 0) return EARN_OK;
   if (!k || !v) { set_error("%s: k and v must not be NULL", who); return EARN_ERR_INVALID_ARG; }
   if (((uintptr_t)k | (uintptr_t)v) & 15) { set_error("%s: k and v must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
-  if (g_validate.load(std::memory_order_relaxed)) {
-    std::vector<int32_t> cu, st((size_t)batch, 0), table;
-    if ((rc = fetch_i32(cu_seqlens, (size_t)batch + 1, cu, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = validate_cu(who, "cu_seqlens", cu, batch, total_tokens, 0x7fffffff)) != EARN_OK) return rc;
-    if (start && (rc = fetch_i32(start, (size_t)batch, st, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = fetch_i32(page_table, (size_t)batch * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    std::vector<long long> rows((size_t)batch), from((size_t)batch), to((size_t)batch);
-    for (int s = 0; s < batch; ++s) {
-      if (st[s] < 0) { set_error("%s: start[%d] = %d is negative", who, s, st[s]); return EARN_ERR_INVALID_ARG; }
-      const int n = cu[s + 1] - cu[s];
-      rows[s] = n > 0 ? (long long)st[s] + n : 0;
-      to[s] = (rows[s] + page_size - 1) / page_size;
-      from[s] = n > 0 ? st[s] / page_size : to[s];
-    }
-    if ((rc = validate_table(who, "page_table", table, batch, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
-    std::vector<int32_t> taken((size_t)n_pages, 0);
-    if ((rc = validate_written(who, "page_table", table, batch, max_pages, from, to, taken)) != EARN_OK) return rc;
-  }
+  if (g_validate.load(std::memory_order_relaxed) && (rc = guarded(who, [&] { return validate_store(who, cu_seqlens, start, page_table, batch, total_tokens, max_pages, n_pages, page_size, stream); })) != EARN_OK) return rc;
   return launch_cache_store(desc, k, v, cu_seqlens, start, batch, total_tokens, k_pages, v_pages, page_table, max_pages, n_pages,
                             page_size, (hipStream_t)stream);
 }
@@ -786,24 +845,7 @@ int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void
   if (weights_out && weight_rows <= 0) { set_error("%s: weight_rows (%d) must be positive", who, weight_rows); return EARN_ERR_INVALID_ARG; }
   const size_t need = decode_paged_workspace_bytes(desc, n_streams, max_cache_len, weights_out != nullptr);
   if ((rc = check_workspace(who, need, workspace, workspace_bytes)) != EARN_OK) return rc;
-  if (g_validate.load(std::memory_order_relaxed)) {
-    std::vector<int32_t> qp, len, table;
-    if ((rc = fetch_i32(q_pos, (size_t)n_streams, qp, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
-    std::vector<long long> rows((size_t)n_streams), from((size_t)n_streams), to((size_t)n_streams);
-    for (int u = 0; u < n_streams; ++u) {
-      if (len[u] < 0) qp[u] = 0;                   // an idle stream's position is not read
-      rows[u] = len[u] < 0 ? 0 : (long long)len[u] + 1;
-      to[u] = (rows[u] + page_size - 1) / page_size;
-      from[u] = rows[u] > 0 ? to[u] - 1 : 0;
-    }
-    if ((rc = validate_positions(who, "q_pos", qp)) != EARN_OK) return rc;
-    if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
-    std::vector<int32_t> taken((size_t)n_pages, 0);
-    if ((rc = validate_written(who, "page_table", table, n_streams, max_pages, from, to, taken)) != EARN_OK) return rc;
-  }
+  if (g_validate.load(std::memory_order_relaxed) && (rc = guarded(who, [&] { return validate_decode_paged(who, q_pos, cache_len, page_table, n_streams, max_cache_len, max_pages, n_pages, page_size, stream); })) != EARN_OK) return rc;
   return launch_decode_paged(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages,
                              page_size, max_cache_len, weights_in, weights_out, weight_rows, out, workspace, (hipStream_t)stream);
 }
@@ -822,8 +864,9 @@ int earn_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, c
   g_err[0] = 0;
   int rc = check_paged_desc(desc, n_streams, who);
   if (rc != EARN_OK) return rc;
-  if (n_streams <= 0 || max_cache_len < 0 || max_cache_len > EARN_MAX_CACHE_LEN || budget <= 0 || weight_rows <= 0) {
-    set_error("%s: n_streams (%d), budget (%d) and weight_rows (%d) must be positive, max_cache_len (%d) in [0, %d]", who, n_streams, budget, weight_rows, max_cache_len, EARN_MAX_CACHE_LEN);
+  if (n_streams <= 0 || max_cache_len < 0 || max_cache_len > EARN_MAX_CACHE_LEN || budget <= 0 || budget > EARN_MAX_CACHE_LEN ||
+      weight_rows <= 0) {
+    set_error("%s: n_streams (%d), budget (%d) and weight_rows (%d) must be positive, max_cache_len (%d) and budget at most %d", who, n_streams, budget, weight_rows, max_cache_len, EARN_MAX_CACHE_LEN);
     return EARN_ERR_INVALID_ARG;
   }
   if (n_first < 0 || n_last < 0 || (long long)n_first + n_last > budget) {
@@ -840,25 +883,7 @@ int earn_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, c
   if (weights_out == weights) { set_error("%s: weights_out must not be weights", who); return EARN_ERR_INVALID_ARG; }
   if (weights_out && weight_rows_out < budget) { set_error("%s: weight_rows_out (%d) is less than budget (%d)", who, weight_rows_out, budget); return EARN_ERR_INVALID_ARG; }
   if ((rc = check_workspace(who, earn_cache_evict_workspace_bytes(desc, n_streams, max_cache_len, budget), workspace, workspace_bytes)) != EARN_OK) return rc;
-  if (g_validate.load(std::memory_order_relaxed)) {
-    std::vector<int32_t> len, table, fresh;
-    if ((rc = fetch_i32(cache_len, (size_t)n_streams, len, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = validate_lengths(who, len, max_cache_len)) != EARN_OK) return rc;
-    if ((rc = fetch_i32(page_table, (size_t)n_streams * max_pages, table, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    if ((rc = fetch_i32(new_table, (size_t)n_streams * new_max_pages, fresh, (hipStream_t)stream, who)) != EARN_OK) return rc;
-    std::vector<long long> rows((size_t)n_streams), kept((size_t)n_streams), zero((size_t)n_streams, 0), to((size_t)n_streams);
-    for (int u = 0; u < n_streams; ++u) {
-      rows[u] = len[u] < 0 ? 0 : len[u];
-      kept[u] = rows[u] < budget ? rows[u] : budget;
-      to[u] = (kept[u] + page_size - 1) / page_size;
-    }
-    if ((rc = validate_table(who, "page_table", table, n_streams, max_pages, n_pages, page_size, rows)) != EARN_OK) return rc;
-    if ((rc = validate_table(who, "new_table", fresh, n_streams, new_max_pages, n_pages, page_size, kept)) != EARN_OK) return rc;
-    std::vector<int32_t> taken((size_t)n_pages, 0);
-    for (int u = 0; u < n_streams; ++u)
-      for (long long i = 0; i * page_size < rows[u]; ++i) taken[table[(size_t)u * max_pages + i]] = 1;
-    if ((rc = validate_written(who, "new_table", fresh, n_streams, new_max_pages, zero, to, taken)) != EARN_OK) return rc;
-  }
+  if (g_validate.load(std::memory_order_relaxed) && (rc = guarded(who, [&] { return validate_evict(who, cache_len, page_table, new_table, n_streams, max_cache_len, budget, max_pages, new_max_pages, n_pages, page_size, stream); })) != EARN_OK) return rc;
   return launch_cache_evict(desc, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages, page_size, max_cache_len,
                             weights, weight_rows, budget, n_first, n_last, new_table, new_max_pages, kept_out, len_out, weights_out,
                             weight_rows_out, (hipStream_t)stream);
@@ -879,7 +904,7 @@ int earn_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t r
     set_error("%s: rows (%d) must be non-negative, vocab (%d) positive, row_stride (%lld) at least vocab", who, rows, vocab, (long long)row_stride);
     return EARN_ERR_INVALID_ARG;
   }
-  if (vocab > 524288) { set_error("%s: vocab (%d) beyond 524288", who, vocab); return EARN_ERR_UNSUPPORTED; }
+  if (vocab > 524288 || rows > (1 << 21)) { set_error("%s: vocab (%d) beyond 524288 or rows (%d) beyond 2^21", who, vocab, rows); return EARN_ERR_UNSUPPORTED; }
   if (rows == 0) return EARN_OK;
   if (!logits || !uniform || !token_out) { set_error("%s: logits, uniform and token_out must not be NULL", who); return EARN_ERR_INVALID_ARG; }
   if ((uintptr_t)logits & (dtype == EARN_F32 ? 3 : 1)) { set_error("%s: logits are not aligned to their type", who); return EARN_ERR_INVALID_ARG; }

@@ -111,18 +111,18 @@ __device__ __forceinline__ int length_of(const int32_t* cache_len, int u, int ma
 
 // The sums of rows [j0, j1) of a (stream, kv head), by the whole workgroup: old sums and the first head's scores are asked for
 // before `states` gives the heads' (reference, 1 / sum) in LDS, and waits for all threads.
-constexpr int kWeightRows = 4 * kPagedThreads;   // of one round
-template <typename States>
+constexpr int kWeightRows = 4 * kPagedThreads;   // of one round of kPagedThreads
+template <int THREADS, typename States>
 __device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, int n, int j0, int j1, const f32x2* state, States states) {
   const int gq = p.hq / p.hkv, tid = threadIdx.x;
   const float* scores = p.scores + ((long long)u * p.hq + c * gq) * p.score_stride;
   const long long to = ((long long)u * p.hkv + c) * p.w_cap;
   bool first = true;
-  for (int jb = j0; jb < j1; jb += kWeightRows) {
+  for (int jb = j0; jb < j1; jb += 4 * THREADS) {
     float w[4], old[4], s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int j = jb + i * kPagedThreads + tid;
+      const int j = jb + i * THREADS + tid;
       w[i] = 0.f;
       old[i] = j < j1 && j < n && p.w_in ? p.w_in[to + j] : 0.f;
       s[i] = j < j1 ? scores[j] : -INFINITY;
@@ -132,7 +132,7 @@ __device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, 
       if (a > 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = jb + i * kPagedThreads + tid;
+          const int j = jb + i * THREADS + tid;
           s[i] = j < j1 ? scores[(long long)a * p.score_stride + j] : -INFINITY;
         }
       }
@@ -142,7 +142,7 @@ __device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, 
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int j = jb + i * kPagedThreads + tid;
+      const int j = jb + i * THREADS + tid;
       if (j < j1) p.w_out[to + j] = old[i] + w[i];
     }
   }
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
     finish_group<T, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, sb * 8, m, l, x);
     if (sb == 0) states[a] = f32x2{m, 1.f / l};
   }
-  if (p.scores && !p.part_o) add_weights(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
+  if (p.scores && !p.part_o) add_weights<kPagedThreads>(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
 }
 
 // bf16: the same on the matrix cores.  Per block of 32 rows a wave computes
@@ -363,12 +363,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
 // 16 consecutive rows have a chunk at different places: a fragment's reads meet no bank twice
 template <int D>
 __device__ __forceinline__ int key_swz(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
-template <int D, int QR, bool STREAMED>
-__global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_mfma_kernel(PagedParams p) {
-  constexpr int KS = D / 32, DB = D / 16, UPR = D / 8, BLK = 32, NV = BLK * UPR / kWave;
+template <int D, int QR, bool STREAMED, int WAVES>
+__global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_mfma_kernel(PagedParams p) {
+  constexpr int THREADS = kWave * WAVES, KS = D / 32, DB = D / 16, UPR = D / 8, BLK = 32, NV = BLK * UPR / kWave;
   union Tile { __bf16 v[BLK * D]; float o[QR][D + 4]; };
-  __shared__ Tile tile[kPagedWaves];
-  __shared__ f32x2 ml[kPagedWaves][QR], states[QR];
+  __shared__ Tile tile[WAVES];
+  __shared__ f32x2 ml[WAVES][QR], states[QR];
   __shared__ __align__(16) __bf16 rot[3][QR + 1][D + 8];   // queries in three terms; row QR of the first: the new key as stored
   __shared__ int pages[kPagedMaxChunk + 2];
   const int gq = p.hq / p.hkv, parts = (gq + QR - 1) / QR;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
   const int j_begin = z * p.chunk, j_end = min(n + 1, j_begin + p.chunk);
   if (n < 0) {                                       // idle: zeros
     if (z == 0)
-      for (int i = tid; i < na * UPR; i += kPagedThreads) {
+      for (int i = tid; i < na * UPR; i += THREADS) {
         const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         Row8<__bf16>::store((__bf16*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + i / UPR)) * D + i % UPR * 8, zero);
       }
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
   const int page0 = (int)p.pg.by_page.div((unsigned)j_begin);
   {
     const int last = (int)p.pg.by_page.div((unsigned)max(j_begin, min(j_end, n) - 1));
-    for (int i = page0 + tid; i <= last; i += kPagedThreads) {   // (a table that is full has no page for row n)
+    for (int i = page0 + tid; i <= last; i += THREADS) {   // (a table that is full has no page for row n)
       const int page = i < p.pg.max_pages ? p.pg.table[(long long)u * p.pg.max_pages + i] : -1;
       pages[i - page0] = (unsigned)page < (unsigned)p.pg.n_pages ? page : -1;
     }
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
   // queries and the new key: 4 rotary pairs of a row per item
   {
     const float pos = (float)p.q_pos[u];
-    for (int item = tid; item < (na + 1) * (D / 8); item += kPagedThreads) {
+    for (int item = tid; item < (na + 1) * (D / 8); item += THREADS) {
       const int row = item / (D / 8), e = item % (D / 8) * 4;
       const bool key = row == na;
       const __bf16* src = (key ? new_k : (const __bf16*)p.q + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a0 + row)) * D) + e;
@@ -499,10 +499,10 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
       there = load_block(kr, (const __bf16*)p.pg.k, wave);
       load_block(vr, (const __bf16*)p.pg.v, wave);
     }
-    for (int blk = wave; blk < n_blocks; blk += kPagedWaves) {
+    for (int blk = wave; blk < n_blocks; blk += WAVES) {
       const int j0 = j_begin + blk * BLK;
       const unsigned stored = there;
-      const bool more = blk + kPagedWaves < n_blocks;
+      const bool more = blk + WAVES < n_blocks;
       const int j_new = blk == n_blocks - 1 && j_end == n + 1 ? n - j0 : BLK;   // the new token's row of the block
       const unsigned mask = j_new < BLK ? stored | 1u << j_new : stored;
       // (opaque: eight addresses a register each, kept over the loop, would not fit)
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
         *(u32x4*)((char*)smv + (key_write ^ key_step(i)) + 1024 * i) = kr[i];
       }
       if (j_new < BLK && lane < UPR) *(u32x4*)(smv + j_new * D + ((lane ^ key_swz<D>(j_new)) << 3)) = *(const u32x4*)&rot[0][QR][lane * 8];
-      if (more) there = load_block(kr, (const __bf16*)p.pg.k, blk + kPagedWaves);
+      if (more) there = load_block(kr, (const __bf16*)p.pg.k, blk + WAVES);
       asm volatile("" ::: "memory");
       // products with the queries' first terms and with what is left of them, apart: an infinite key element gives its
       // infinity with the first term, and NaN where the terms differ in sign
@@ -547,7 +547,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
         asm volatile("" ::: "memory");
         if (j_new < BLK && lane < UPR) *(u32x4*)(smv + j_new * D + ((lane ^ short_v_swz<D>(j_new)) << 3)) = newest;
       }
-      if (more) load_block(vr, (const __bf16*)p.pg.v, blk + kPagedWaves);
+      if (more) load_block(vr, (const __bf16*)p.pg.v, blk + WAVES);
       if (mask != 0xffffffffu) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -597,13 +597,13 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
     if (quad == 0) ml[wave][r16] = f32x2{mrow, lrow};
   }
   __syncthreads();
-  for (int i = tid; i < na * UPR; i += kPagedThreads) {
+  for (int i = tid; i < na * UPR; i += THREADS) {
     const int a = i / UPR, e = (i % UPR) * 8;
     float m = -INFINITY, l = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) m = fmaxf(m, ml[w][a][0]);
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml[w][a][0]);
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w >= n_blocks) continue;                    // a wave without rows: its tile holds nothing
       const float f = ml[w][a][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][a][0] - m);
       l += f * ml[w][a][1];
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(kPagedThreads, D == 64 ? 3 : 2) void paged_decode_m
     finish_group<__bf16, D>(p, (long long)u * p.hq, c * gq + a0 + a, z, e, m, l, x);
     if (e == 0) states[a] = f32x2{m, 1.f / l};
   }
-  if (p.scores && !p.part_o) add_weights(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
+  if (p.scores && !p.part_o) add_weights<THREADS>(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
 }
 
 // Joins the splits' states.  Blocks x < Hq / Hkv of a (kv head, stream) give one query head's output each: 256 / (D / 8) lanes
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p)
   const int j0 = (int)(blockIdx.x - gq) * kWeightRows, j1 = min(min(n + 1, j0 + kWeightRows), p.w_cap);
   if (j0 >= j1) return;
   __shared__ f32x2 state[kMaxGroup];
-  add_weights(p, u, c, n, j0, j1, state, [&]() {
+  add_weights<kJoinThreads>(p, u, c, n, j0, j1, state, [&]() {
     for (int a = tid / kWave; a < gq; a += kJoinThreads / kWave) {   // a wave per head
       const f32x2* split = (const f32x2*)p.part_ml + (head0 + a) * p.n_splits;
       float m = -INFINITY, l = 0.f;
@@ -956,6 +956,7 @@ static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_l
   if (rows <= 640) chunk = rows;
   if (forced > 0) chunk = forced < kPagedMaxChunk ? forced : kPagedMaxChunk;
   if (chunk > rows) chunk = rows;
+  if (chunk < rows / 65535 + 1) chunk = rows / 65535 + 1;   // a grid dimension
   pl.chunk = (int)((chunk + 63) / 64 * 64);
   pl.n_splits = (int)((rows + pl.chunk - 1) / pl.chunk);
   pl.score_stride = (int)((rows + 31) / 32 * 32);   // whole blocks of rows
@@ -997,16 +998,28 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   // streams of 8192-32768 rows 237 -> 217 us; 256 streams of 100-500 rows, 63 MB, 19.2 -> 19.6.
   const bool streamed = 2ll * n_streams * p.hkv * max_len * desc->head_dim * (mfma ? 2 : 4) > (256ll << 20);
   const int gq = p.hq / p.hkv, g = paged_heads(desc), parts = paged_parts(desc);
+  // Eight waves share the rows of a stream that is not split, where no other workgroup would fill the CU: us, 32 streams of 256-528
+  // rows, 14 / 2 heads of 64, 11.4 -> 9.5; 8 of 500, 32 / 8 heads, 13.3 -> 11.8; 16 of 100-300 11.9 -> 11.0; but 256 of 100-500, 12 / 2 heads
+  // (512 workgroups), 20.3 -> 25.4, and split caches gain nothing (one of 65521 rows 24.3 -> 25.7).
+  const bool wide = pl.n_splits == 1 && (long long)p.hkv * parts * n_streams <= 256 && pl.chunk > 128;
   // splits last: consecutive workgroups go to the XCDs in turn, and with two splits side by side every other XCD had short ones only
   // (64 streams of 256-2080 rows, 32 heads, two splits: 277 us, this way 209)
   const dim3 grid(p.hkv * parts, n_streams, pl.n_splits);
   for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
-    if (mfma && g == 8 && streamed) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8, true>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (mfma && g == 8) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 8, false>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (mfma && streamed) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16, true>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (mfma) hipLaunchKernelGGL((paged_decode_mfma_kernel<D, 16, false>), grid, dim3(kPagedThreads), 0, stream, p);
+    auto mfma_launch = [&](auto qr, auto nt, auto waves) {
+      hipLaunchKernelGGL((paged_decode_mfma_kernel<D, decltype(qr)::value, decltype(nt)::value, decltype(waves)::value>), grid, dim3(kWave * decltype(waves)::value), 0, stream, p);
+    };
+    constexpr std::integral_constant<int, 4> four;
+    constexpr std::integral_constant<int, 8> eight;
+    constexpr std::integral_constant<int, 16> sixteen;
+    if (mfma && g == 8 && streamed) mfma_launch(eight, std::true_type{}, four);
+    else if (mfma && streamed) mfma_launch(sixteen, std::true_type{}, four);
+    else if (mfma && g == 8 && wide) mfma_launch(eight, std::false_type{}, eight);
+    else if (mfma && wide) mfma_launch(sixteen, std::false_type{}, eight);
+    else if (mfma && g == 8) mfma_launch(eight, std::false_type{}, four);
+    else if (mfma) mfma_launch(sixteen, std::false_type{}, four);
     else if constexpr (sizeof(T) == 2) return;
     else if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
     else if (g == 2) hipLaunchKernelGGL((paged_decode_kernel<T, D, 2>), grid, dim3(kPagedThreads), 0, stream, p);

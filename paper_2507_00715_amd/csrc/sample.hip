@@ -91,10 +91,8 @@ struct Weights {
   float bins;         // bins per unit of logit
   double scale;       // 128 log2(e) / T
   const double* power;
-  __device__ __forceinline__ double real(float l) const { return power_of(fmax(((double)l - (double)best) * scale, -1100.0 * kExpSteps)); }
-  // of an entry that is not in the last bin
-  __device__ __forceinline__ u64 of_near(float l) const { return whole(power_of(((double)l - (double)best) * scale)); }
-  __device__ __forceinline__ double power_of(double t) const {   // 2^(t / kExpSteps)
+  __device__ __forceinline__ double real(float l) const {
+    const double t = fmax(((double)l - (double)best) * scale, -1100.0 * kExpSteps);
     const double shifted = t + 0x1.8p52, r = t - (shifted - 0x1.8p52);
     const int n = (int)(unsigned)__double_as_longlong(shifted);
     constexpr double c = 0.69314718055994530942 / kExpSteps;
@@ -535,7 +533,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   if (top_p < 1.f) {
     u64 all = 0;
     auto add_mass = [&](float l, int b) {
-      const u64 w = wt.of_near(l);
+      const u64 w = wt.of(l);
       atomicAdd(&sm.mass[b], w);
       all += w;
     };

@@ -158,6 +158,17 @@ def test_uniform_numbers_outside_their_range_and_odd_parameters():
     assert token == [0, 0, 0, 0, 0, 5, 5, 5] and count == [1, 1, 1, 1, 1, 10, 10, 10]
 
 
+def test_temperatures_and_logits_of_the_smallest_numbers():
+    """Differences of logits over temperatures that both lie at the lower end of fp32, and temperatures at the upper end."""
+    B = _B()
+    x = torch.arange(9, dtype=torch.float32).repeat(6, 1) * 1e-44
+    t = [1e-44, 3e-44, 1e-45, 1e-38, 1e38, 3e-37]
+    for params in (dict(), dict(top_p=[0.8] * 6), dict(top_k=[4] * 6), dict(min_p=[0.1] * 6)):
+        check(B, x, [0.0371, 0.4001, 0.9001, 0.3001, 0.6003, 0.9502], temperature=t, **params)
+    far = torch.tensor([[0.0, -1e-37, -2e-37, -1e-36, -5e-36, -1e38]] * 4)
+    check(B, far, [0.1, 0.7, 0.95, 0.9999], temperature=[1e-37, 2e-37, 1e-38, 1e-45], top_p=[0.99] * 4)
+
+
 def test_frequencies_follow_the_weights():
     """The draw with u = (i + 1/2) / n takes token t round(n p_t) times, up to one each way for its two borders."""
     B = _B()

@@ -41,7 +41,7 @@ def test_decode_refusals():
     refused(call(desc=_desc(hq=129, hkv=1)), B.EARN_ERR_UNSUPPORTED, "query heads")
     refused(call(S=70000), B.EARN_ERR_UNSUPPORTED, "streams")
     for kw in (dict(q=None), dict(S=0), dict(pages=None), dict(table=None), dict(length=None), dict(page=0), dict(bound=-1),
-               dict(bound=(1 << 30) + 1), dict(w_in=FAKE), dict(w_out=FAKE), dict(out=None), dict(q=264), dict(out=258)):
+               dict(bound=(1 << 26) + 1), dict(w_in=FAKE), dict(w_out=FAKE), dict(out=None), dict(q=264), dict(out=258)):
         refused(call(**kw), B.EARN_ERR_INVALID_ARG, "earn_decode_attn_paged")
     need = B.earn_decode_paged_workspace_bytes(_desc(), 2, 100000, False)
     more = B.earn_decode_paged_workspace_bytes(_desc(), 2, 100000, True)
@@ -60,7 +60,7 @@ def test_evict_refusals():
                                         first, last, fresh, new_pages, kept, len_out, w_out, w_rows_out, None, 0, None)
 
     refused(call(desc=_desc(d=256)), B.EARN_ERR_UNSUPPORTED, "head_dim")
-    for kw in (dict(pages=None), dict(length=None), dict(S=0), dict(bound=-1), dict(w=None), dict(w_rows=99), dict(budget=0), dict(first=-1),
+    for kw in (dict(pages=None), dict(length=None), dict(S=0), dict(bound=-1), dict(w=None), dict(w_rows=99), dict(budget=0), dict(budget=(1 << 26) + 1, new_pages=1 << 30), dict(first=-1),
                dict(last=-1), dict(first=60), dict(fresh=None), dict(new_pages=3), dict(kept=None), dict(len_out=None), dict(w_out=FAKE),
                dict(w_out=512, w_rows_out=63)):
         refused(call(**kw), B.EARN_ERR_INVALID_ARG, "earn_cache_evict")
@@ -72,6 +72,7 @@ def test_sample_refusals():
 
     refused(call(dtype=2), B.EARN_ERR_UNSUPPORTED, "dtype")
     refused(call(vocab=524289, stride=524289), B.EARN_ERR_UNSUPPORTED, "vocab")
+    refused(call(rows=(1 << 21) + 1), B.EARN_ERR_UNSUPPORTED, "rows")
     for kw in (dict(logits=None), dict(logits=258), dict(stride=99), dict(rows=-1), dict(vocab=0), dict(u=None), dict(token=None)):
         refused(call(**kw), B.EARN_ERR_INVALID_ARG, "earn_sample")
     assert call(rows=0, logits=None) == B.EARN_OK
