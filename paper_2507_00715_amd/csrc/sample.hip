@@ -14,8 +14,8 @@
 // memory instead).  What bounds a row is how many vector instructions its entries take on their one CU, so the passes over all
 // entries are few and short:
 //   - the largest logit;
-//   - top-k up to kSmallK: a histogram over (l_max - l) / T of the largest entry of every 16 bytes gives a border that at least k
-//     entries reach, and few more: those are listed, and the rest happens in the list;
+//   - top-k up to kSmallK: the largest entries of every 16 bytes (of longer rows, of some of them together) stay in LDS; a histogram of them over (l_max - l) / T gives a border
+//     that at least k entries reach, and few more: those are listed, and the rest happens in the list;
 //   - else top-k: a histogram of all entries; top-p: one of their weights; the few entries of the bin in which a beginning ends are
 //     ranked among each other;
 //   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept;
@@ -32,6 +32,7 @@ constexpr int kBinsPerUnit = 64;
 constexpr int kFraction = 44;          // exp(-31.98) 2^44 < 1/2: the last bin's weights are all zero
 constexpr int kListMax = 1024;
 constexpr int kSmallK = 512;           // largest top-k that is worked out in the list
+constexpr int kGroups = 16384;         // groups of entries whose largest are kept in LDS
 constexpr int kExpSteps = 128;         // of the table of powers of two
 
 struct SampleParams {
@@ -55,6 +56,7 @@ struct SampleSmem {
   u64 list_w[kListMax];
   u64 list_key[kListMax];        // (order key, ~index): larger is earlier in the order
   u64 sorted[kSmallK];
+  float group_best[WAVES > 4 ? kGroups : 4 * 4 * kWave];   // a lane's 16 bytes of one unit, or of the next 2, 4, ... units of longer rows
   int by_index[kSmallK];
   double power[kExpSteps];       // 2^(i / kExpSteps)
   float queue[WAVES][2 * kWave];
@@ -406,8 +408,22 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
   for (int i = tid; i < kExpSteps; i += THREADS) sm.power[i] = exp2((double)i / kExpSteps);
   for (int i = tid; i < kBins; i += THREADS) { sm.mass[i] = 0; sm.count[i] = 0; }
+  typedef Run<T, WAVES> R;
+  const bool few = top_k > 1 && top_k <= kSmallK;
+  int shift = 0;                                  // 2^shift units a group
+  while ((run.units + (1 << shift) - 1) >> shift > (int)(sizeof(sm.group_best) / sizeof(float)) / THREADS) ++shift;
+  float* group_best = sm.group_best + wave * ((run.units + (1 << shift) - 1) >> shift) * kWave + lane;
   float best = -INFINITY;
-  run.each([&](int, float l) { best = l > best ? l : best; });
+  if (few) {                                      // the groups' largest stay: a thread reads what it wrote
+    run.each_unit([&](int at, const u32x4& x) {
+      const int i = (at - run.begin) / (kWave * R::E);
+      float most = i & ((1 << shift) - 1) ? group_best[(i >> shift) * kWave] : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) { const float l = run.element(x, e); most = l > most ? l : most; }
+      group_best[(i >> shift) * kWave] = most;
+      best = fmaxf(best, most);
+    });
+  } else run.each([&](int, float l) { best = l > best ? l : best; });
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) best = fmaxf(best, __shfl_xor(best, o, kWave));
   if (lane == 0) sm.wave_best[wave] = best;
@@ -450,7 +466,6 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   wt.bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
   wt.power = sm.power;
   const Draw d{(double)u, (double)temperature, top_p, min_p > 0.f ? (double)fminf(min_p, 1.f) : 0.0, top_k};
-  typedef Run<T, WAVES> R;
   Beginning kept{-INFINITY, -1};
   auto list_key = [&](int i, float l) {
     const int at = atomicAdd(&sm.n_list, 1);
@@ -458,16 +473,27 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   };
   bool limited = false;
   if (top_k > 0) {
-    if (top_k <= kSmallK) {
-      run.each_unit([&](int, const u32x4& x) {
-        float most = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < R::E; ++e) { const float l = run.element(x, e); most = l > most ? l : most; }
+    if (few) {
+      const int groups = (run.n_units + (1 << shift) - 1) >> shift;
+#pragma unroll 4
+      for (int i = 0; i < groups; ++i) {
+        const float most = group_best[i * kWave];
         if (most > -INFINITY) atomicAdd(&sm.count[wt.bin(most)], 1);
-      });
+      }
       const int bin = find_bin<false>(sm, top_k, 0);
       if (bin < kBins - 1) {
-        run.each([&](int i, float l) { if (wt.bin(l) <= bin) list_key(i, l); });
+        for (int i = 0; i < groups; ++i) {
+          if (wt.bin(group_best[i * kWave]) > bin) continue;
+          for (int k = i << shift; k < min((i + 1) << shift, run.n_units); ++k) {
+            const int at = run.index(k, 0);
+            const u32x4 x = run.load_at(at);
+#pragma unroll
+            for (int e = 0; e < R::E; ++e) {
+              const float l = run.element(x, e);
+              if (wt.bin(l) <= bin) list_key(at + e, l);
+            }
+          }
+        }
         __syncthreads();
         const int n = sm.n_list;
         if (n <= kListMax) { draw_from_list(p, wt, d, n, sm); return; }
