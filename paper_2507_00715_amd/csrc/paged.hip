@@ -37,7 +37,9 @@ __device__ __forceinline__ int capacity_of(const Pages& pg) {   // rows that a t
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// store: 4 times 16 bytes of a K and a V row per thread
+// store: a copy, four times 16 bytes of a K and a V row per thread, all asked for before the places are looked up.  256 prompts of
+// 64-1024 rows, 2 heads of 128 (180 MB read and written): 39 us, 4.6 TB/s, of 35 that a large copy takes.  (One unit a thread 48; a
+// search for every unit's sequence instead of one a workgroup 45.)
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kStoreUnits = 4;
 template <typename T, int D>
@@ -87,6 +89,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restric
 // ------------------------------------------------------------------------------------------------------------------
 // decode
 // ------------------------------------------------------------------------------------------------------------------
+// The vector form (fp32): a row is spread over d / 8 lanes, a wave takes whole rows, every lane keeps softmax states of up to 8 query
+// heads over its share of them (larger groups: a workgroup each for 8 heads, which read the rows again).  Bound by HBM, with the
+// vector ALU near it: one stream of 32768 rows, 32 / 8 heads of 128 (268 MB), 64 us, 4.2 TB/s.
 constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / kWave;
 constexpr int kPagedMaxChunk = 2048;   // rows of a split: its page numbers lie in LDS
 
@@ -360,6 +365,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
 // values pass through one swizzled LDS tile of the wave's own: they leave memory whole lines at a time, as they lie there (key
 // fragments straight from memory touch half lines, which loads that leave nothing in the caches then fetch twice).  While a
 // block is worked on, the next one's rows are on their way: each half is asked for as soon as this block's is in LDS.
+// Bound by HBM: 16 streams of 8192-32768 rows, 32 / 8 heads of 128 (1.28 GB), 216 us, 5.9 TB/s; loads of the same addresses and
+// nothing else take 188.  (The vector form 292; key fragments straight from memory, three waves a SIMD instead of two, 225.)
 // 16 consecutive rows have a chunk at different places: a fragment's reads meet no bank twice
 template <int D>
 __device__ __forceinline__ int key_swz(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
@@ -442,7 +449,7 @@ __global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_m
   // A block as it lies in memory: unit lane + 64 i of its rows, 16 bytes each.  Every unit is loaded, those of rows that are not
   // there from some row that is in the pool.  Returns which rows are there.
   // Whole blocks over pages of a multiple of 16 rows: 16 rows lie in one page, one behind the other, and a wave looks their pages
-  // up once (one row at a time, a block took 590 vector instructions, now 330).
+  // up once (one row at a time, a block took 590 vector instructions; 280 now).
   constexpr int RPI = kWave / UPR;                    // rows of 64 units
   const bool by_sixteen = p.pg.page_size % 16 == 0;
   auto load_block = [&](u32x4 (&x)[NV], const __bf16* pool, int blk) {
@@ -616,7 +623,8 @@ __global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_m
   if (p.scores && !p.part_o) add_weights<THREADS>(p, u, c, n, 0, min(n + 1, p.w_cap), states, [] { __syncthreads(); });
 }
 
-// Joins the splits' states.  Blocks x < Hq / Hkv of a (kv head, stream) give one query head's output each: 256 / (D / 8) lanes
+// Joins the splits' states.  Bound by its trips to memory, one behind the other: 128 splits of 12 heads with the weights of 65521 rows
+// 7 us (83 with a thread walking all splits).  Blocks x < Hq / Hkv of a (kv head, stream) give one query head's output each: 256 / (D / 8) lanes
 // share the splits, then meet in LDS.  The blocks behind them give 1024 rows' weights each.
 constexpr int kJoinThreads = kPagedThreads, kMaxGroup = 128;
 template <typename T, int D>
@@ -705,7 +713,8 @@ __device__ __forceinline__ unsigned weight_key(float w) {
 // them, whose keys stay in registers (ROWS = 0: any number, read again in every pass).  Weights crowd: most of the first histogram's
 // additions go to a few neighbouring bins, so that eight copies of it, a lane's by its number, take them in turn.  The rows
 // that agree in the first 11 bits are listed, a few hundred as a rule, and the other digits come from the list.  One workgroup
-// does all of it, so what bounds it is how often it touches every row: the first histogram, the list, two counts, the result.
+// does all of it, so what bounds it is the vector instructions that every row takes in its few passes: the first histogram, the list,
+// two counts, the result.  8 x 8 heads of 32768 rows 29 us (one bit a pass, rows read again, 252), 64 x 2 of 1024-2048 rows 10 (25).
 constexpr int kDigitBins = 2048, kDigitCopies = 8, kDigitList = 4096;
 struct SelectSmem {
   int bins[kDigitBins * kDigitCopies];
@@ -867,7 +876,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
   });
 }
 
-// 16 bytes of a K and a V row per thread
+// 16 bytes of a K and a V row per thread.  A gathering copy: 8 x 8 heads x 4096 rows of 128 (268 MB read and written) 55 us, 4.9 TB/s, what
+// a large copy reaches; 64 x 2 x 1000 rows (131 MB) 25.5.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   constexpr int UPR = D * (int)sizeof(T) / 16;

@@ -14,8 +14,9 @@
 // memory instead).  What bounds a row is how many vector instructions its entries take on their one CU, so the passes over all
 // entries are few and short:
 //   - the largest logit;
-//   - top-k up to kSmallK: the largest entries of every 16 bytes (of longer rows, of some of them together) stay in LDS; a histogram of them over (l_max - l) / T gives a border
-//     that at least k entries reach, and few more: those are listed, and the rest happens in the list;
+//   - top-k up to kSmallK: the largest entries of every 16 bytes (of longer rows, of some of them together) stay in LDS; a histogram of
+//     them over (l_max - l) / T gives a border that at least k entries reach, and few more: those are listed, and the rest happens in the
+//     list;
 //   - else top-k: a histogram of all entries; top-p: one of their weights; the few entries of the bin in which a beginning ends are
 //     ranked among each other;
 //   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept;
