@@ -487,8 +487,8 @@ size_t earn_cache_evict_workspace_bytes(const earn_attn_desc* desc, int32_t n_st
  * kept w_0 + ... + w_t exceed u times the weight W of all kept.  T not above 0, or p not above 0: the first token of the order.
  * NaN counts as -inf; -inf is never drawn or kept; with infinite logits those alone are kept, at equal weights; a row without
  * any finite or infinite logit gives token -1, log-probability -inf, 0 kept.  u is cut to [0, 1).
- * Weights are held as 64-bit integers, w_i 2^44 rounded: a token of less than 2^-45 of the best one's probability is never
- * drawn, and no order of summation decides.
+ * Weights are worked out to 2^-46 of themselves and held as 64-bit integers, w_i 2^44 rounded: a token of less than 2^-45 of the
+ * best one's probability is never drawn, and no order of summation decides.
  *   logits       [rows, vocab], dtype EARN_F32 or EARN_BF16, row r at logits + r * row_stride elements (any row_stride >= vocab)
  *   uniform      [rows] fp32
  *   temperature, top_p, min_p  [rows] fp32, top_k  [rows] int32; each may be NULL (1, all, all, all)

@@ -767,15 +767,11 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
   const long long pair = (long long)u * p.pg.hkv + c;
   const float* w = p.w_in + pair * p.w_cap;
   int32_t* kept = p.kept + pair * p.budget;
-  float* w_out = p.w_out ? p.w_out + pair * p.w_out_cap : nullptr;
   const int m = min(n, p.budget);
   for (int i = max(m, 0) + tid; i < p.budget; i += kSelectThreads) kept[i] = -1;
   if (n < 0) return;
   if (n <= p.budget) {
-    for (int i = tid; i < n; i += kSelectThreads) {
-      kept[i] = i;
-      if (w_out) w_out[i] = w[i];
-    }
+    for (int i = tid; i < n; i += kSelectThreads) kept[i] = i;
     return;
   }
   const int lo = p.first, hi = n - p.last, need = p.budget - p.first - p.last;   // rows [lo, hi) compete for `need` places
@@ -787,14 +783,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
 #pragma unroll
     for (int i = 0; i < PER; ++i) held[i] = __float_as_uint(begin + i * kWave + lane < end ? w[begin + i * kWave + lane] : 0.f);
   }
-  for (int i = tid; i < p.first; i += kSelectThreads) {
-    kept[i] = i;
-    if (w_out) w_out[i] = w[i];
-  }
-  for (int i = tid; i < p.last; i += kSelectThreads) {
-    kept[p.budget - p.last + i] = hi + i;
-    if (w_out) w_out[p.budget - p.last + i] = w[hi + i];
-  }
+  for (int i = tid; i < p.first; i += kSelectThreads) kept[i] = i;
+  for (int i = tid; i < p.last; i += kSelectThreads) kept[p.budget - p.last + i] = hi + i;
   if (need <= 0) return;
   for (int i = tid; i < kDigitBins * kDigitCopies / 4; i += kSelectThreads) *(u32x4*)&sm.bins[4 * i] = u32x4{0u, 0u, 0u, 0u};
   if (tid == 0) sm.listed = 0;
@@ -867,16 +857,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
     for (int drop = __popcll(same) - left; drop > 0; --drop) same &= ~(1ull << (63 - __builtin_clzll(same)));
     left -= __popcll(same);
     mask |= same;
-    if (mask >> lane & 1) {
-      const int to = at + __popcll(mask & ((1ull << lane) - 1));
-      kept[to] = j;
-      if (w_out) w_out[to] = w[j];
-    }
+    if (mask >> lane & 1) kept[at + __popcll(mask & ((1ull << lane) - 1))] = j;
     at += __popcll(mask);
   });
 }
 
-// 16 bytes of a K and a V row per thread.  A gathering copy: 8 x 8 heads x 4096 rows of 128 (268 MB read and written) 55 us, 4.9 TB/s, what
+// 16 bytes of a K and a V row per thread, and the kept rows' sums.  A gathering copy: 8 x 8 heads x 4096 rows of 128 (268 MB read and written) 55 us, 4.9 TB/s, what
 // a large copy reaches; 64 x 2 x 1000 rows (131 MB) 25.5.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
@@ -887,8 +873,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
     p.len_out[u] = min(n, p.budget);
   }
   if (i >= p.budget) return;
-  const int r = p.kept[((long long)u * p.pg.hkv + c) * p.budget + i];
+  const long long pair = (long long)u * p.pg.hkv + c;
+  const int r = p.kept[pair * p.budget + i];
   if (r < 0) return;
+  if (unit == 0 && p.w_out) p.w_out[pair * p.w_out_cap + i] = p.w_in[pair * p.w_cap + r];
   int in_old;
   const int old = page_of_row(p.pg, u, r, in_old);
   const int at = (int)p.pg.by_page.div((unsigned)i), page = p.new_table[(long long)u * p.new_pages + at];

@@ -34,7 +34,7 @@ constexpr int kFraction = 44;          // exp(-31.98) 2^44 < 1/2: the last bin's
 constexpr int kListMax = 1024;
 constexpr int kSmallK = 512;           // largest top-k that is worked out in the list
 constexpr int kGroups = 16384;         // groups of entries whose largest are kept in LDS
-constexpr int kExpSteps = 128;         // of the table of powers of two
+constexpr int kExpBits = 9, kExpSteps = 1 << kExpBits;   // of the table of powers of two
 
 struct SampleParams {
   const void* logits; long long row_stride;
@@ -59,51 +59,66 @@ struct SampleSmem {
   u64 sorted[kSmallK];
   float group_best[WAVES > 4 ? kGroups : 4 * 4 * kWave];   // a lane's 16 bytes of one unit, or of the next 2, 4, ... units of longer rows
   int by_index[kSmallK];
-  double power[kExpSteps];       // 2^(i / kExpSteps)
+  double power[kExpSteps];
   float queue[WAVES][2 * kWave];
   u64 wave_mass[WAVES];
   int wave_count[WAVES];
   float wave_best[WAVES];
   int wave_at[WAVES];
-  int n_list, bin, found_index, before_count;
+  int n_list, n_groups, bin, found_index, before_count;
   float found_value;
   u64 before_mass, kept_mass[WAVES];
   int kept_count[WAVES];
 };
 
-template <typename X>
-__device__ __forceinline__ X wave_sum(X x) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o, kWave);
-  return x;
+// Sums over a wave without trips through LDS: inclusive prefix sums inside rows of 16 lanes, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 x) {
+  return (u64)(unsigned)moved<CTRL, ROWS>((int)(x >> 32)) << 32 | (unsigned)moved<CTRL, ROWS>((int)x);
 }
 template <typename X>
-__device__ __forceinline__ X wave_scan(X x, int lane) {   // inclusive
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const X y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
+__device__ __forceinline__ X wave_scan(X x) {   // inclusive; all lanes
+  x += moved<0x111, 0xf>(x);   // row_shr 1, 2, 4, 8
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);   // lane 15 of rows 0 and 2 to the rows behind them
+  x += moved<0x143, 0xc>(x);   // lane 31 to the second half
   return x;
 }
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+__device__ __forceinline__ u64 last_lane(u64 x) { return (u64)(unsigned)last_lane((int)(x >> 32)) << 32 | (unsigned)last_lane((int)x); }
+template <typename X>
+__device__ __forceinline__ X wave_sum(X x) { return last_lane(wave_scan(x)); }
 
-// Weights of a row.  exp((l - best) / T) = 2^(n / 128) exp(r ln 2 / 128) with n whole and |r| <= 1/2: a table and the exponential series
-// to the fourth power, whose next term is below 2^-49.
+// Weights of a row, as doubles times 2^kFraction.  exp((l - best) / T) = 2^(n / 512) exp(r ln 2 / 512) with n whole and |r| <= 1/2: a
+// table and the exponential series to the third power, whose next term is below 2^-46.
 struct Weights {
   float best;         // the largest logit
   float bins;         // bins per unit of logit
-  double scale;       // 128 log2(e) / T
-  const double* power;
+  double scale;       // kExpSteps log2(e) / T
+  double c1, c2, c3;  // of the series, in scalar registers
+  const double* power;   // 2^(i / kExpSteps), times 2^kFraction
+  __device__ __forceinline__ void init(float best_, float temperature, const double* power_) {
+    best = best_;
+    bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
+    scale = kExpSteps * 1.4426950408889634074 / (double)temperature;
+    power = power_;
+    constexpr double c = 0.69314718055994530942 / kExpSteps;
+    c1 = c; c2 = c * c / 2; c3 = c * c * c / 6;
+    asm("" : "+s"(c1), "+s"(c2), "+s"(c3));
+  }
   __device__ __forceinline__ double real(float l) const {
     const double t = fmax(((double)l - (double)best) * scale, -1100.0 * kExpSteps);
     const double shifted = t + 0x1.8p52, r = t - (shifted - 0x1.8p52);
     const int n = (int)(unsigned)__double_as_longlong(shifted);
-    constexpr double c = 0.69314718055994530942 / kExpSteps;
-    const double e = __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, c * c * c * c / 24, c * c * c / 6), c * c / 2), c), 1.0);
-    return __builtin_amdgcn_ldexp(power[n & (kExpSteps - 1)] * e, n >> 7);
+    const double e = __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, c3, c2), c1), 1.0);
+    return __builtin_amdgcn_ldexp(power[n & (kExpSteps - 1)] * e, n >> kExpBits);
   }
-  static __device__ __forceinline__ u64 whole(double w) {   // w 2^kFraction, rounded; w <= 1
-    return (u64)__double_as_longlong(__builtin_fma(w, (double)(1ull << kFraction), 0x1p52)) & 0xfffffffffffffull;
+  static __device__ __forceinline__ u64 whole(double w) {   // rounded; w <= 2^kFraction
+    return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull;
   }
   __device__ __forceinline__ u64 of(float l) const { return whole(real(l)); }
   // monotone in l: rounding keeps the order of differences and products
@@ -185,14 +200,13 @@ struct Beginning {
   __device__ __forceinline__ bool has(int i, float l) const { return l > value || (l == value && i <= index); }
 };
 
-// The bin in which the k-th entry lies (by sm.count), or the one that reaches `mass` (by sm.mass), and what the bins before it hold;
-// kBins: none.  Called by all threads.
+// The bin in which the k-th entry lies (by sm.count), or in which the weights reach `share` (at most 1) of their sum (by sm.mass; that
+// weight to `target`), and what the bins before it hold in sm; kBins: none.  Called by all threads.
 template <bool BY_MASS, int WAVES>
-__device__ __forceinline__ int find_bin(SampleSmem<WAVES>& sm, int k, u64 mass) {
+__device__ __forceinline__ int find_bin(SampleSmem<WAVES>& sm, int k, double share, u64& target_mass) {
   constexpr int THREADS = kWave * WAVES, PER = kBins / THREADS;
   typedef typename std::conditional<BY_MASS, u64, int>::type Sum;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const Sum target = BY_MASS ? (Sum)mass : (Sum)k;
   __syncthreads();
   Sum own[PER], sum = 0;
 #pragma unroll
@@ -200,12 +214,20 @@ __device__ __forceinline__ int find_bin(SampleSmem<WAVES>& sm, int k, u64 mass) 
     if constexpr (BY_MASS) own[i] = sm.mass[PER * tid + i]; else own[i] = sm.count[PER * tid + i];
     sum += own[i];
   }
-  const Sum upto = wave_scan(sum, lane);
+  const Sum upto = wave_scan(sum);
   if (lane == kWave - 1) { if constexpr (BY_MASS) sm.wave_mass[wave] = upto; else sm.wave_count[wave] = upto; }
-  if (tid == 0) { sm.bin = kBins; sm.n_list = 0; }
+  if (tid == 0) { sm.bin = kBins; sm.n_list = sm.n_groups = 0; }
   __syncthreads();
-  Sum before = upto - sum;
-  for (int i = 0; i < wave; ++i) { if constexpr (BY_MASS) before += sm.wave_mass[i]; else before += sm.wave_count[i]; }
+  Sum before = upto - sum, all = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    Sum w;
+    if constexpr (BY_MASS) w = sm.wave_mass[i]; else w = sm.wave_count[i];
+    before += i < wave ? w : 0;
+    all += w;
+  }
+  Sum target;
+  if constexpr (BY_MASS) target = target_mass = min(max((u64)ceil(share * (double)all), (u64)1), all); else target = k;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     if (before < target && before + own[i] >= target) {
@@ -236,12 +258,12 @@ __device__ __forceinline__ void find_equal(const R& run, float value, int r, Sam
       int here = 0;
 #pragma unroll
       for (int e = 0; e < R::E; ++e) here += run.element(x, e) == value ? 1 : 0;
-      const int upto = at + wave_scan(here, lane);
+      const int upto = at + wave_scan(here);
       int own = upto - here;
 #pragma unroll
       for (int e = 0; e < R::E; ++e)
         if (run.element(x, e) == value && ++own == r) sm.found_index = run.index(i, e);
-      at = __shfl(upto, kWave - 1, kWave);
+      at = last_lane(upto);
     }
   }
   __syncthreads();
@@ -300,7 +322,7 @@ __device__ __forceinline__ u64 block_sum(u64 x, SampleSmem<WAVES>& sm) {
 }
 
 // What the threads need of the row's parameters to finish it.
-struct Draw { double u, temperature; float top_p; double least; int top_k; };
+struct Draw { double u, temperature; float top_p; double least; int top_k; };   // least: min-p's weight, times 2^kFraction
 // u W falls to the first sum that reaches this
 __device__ __forceinline__ u64 reach_of(double u, u64 total) { return min((u64)(u * (double)total) + 1, total); }
 __device__ __forceinline__ float logprob_of(float l, float best, double temperature, u64 total) {
@@ -312,7 +334,7 @@ __device__ __forceinline__ float logprob_of(float l, float best, double temperat
 template <int WAVES>
 __device__ __forceinline__ u64 block_scan(u64 x, u64& base, SampleSmem<WAVES>& sm) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  x = wave_scan(x, lane);
+  x = wave_scan(x);
   __syncthreads();
   if (lane == kWave - 1) sm.wave_mass[wave] = x;
   __syncthreads();
@@ -407,7 +429,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
   float u = p.uniform[r];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-  for (int i = tid; i < kExpSteps; i += THREADS) sm.power[i] = exp2((double)i / kExpSteps);
+  for (int i = tid; i < kExpSteps; i += THREADS) sm.power[i] = exp2((double)i / kExpSteps + kFraction);
   for (int i = tid; i < kBins; i += THREADS) { sm.mass[i] = 0; sm.count[i] = 0; }
   typedef Run<T, WAVES> R;
   const bool few = top_k > 1 && top_k <= kSmallK;
@@ -462,12 +484,10 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   }
 
   Weights wt;
-  wt.best = best;
-  wt.scale = kExpSteps * 1.4426950408889634074 / (double)temperature;
-  wt.bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
-  wt.power = sm.power;
-  const Draw d{(double)u, (double)temperature, top_p, min_p > 0.f ? (double)fminf(min_p, 1.f) : 0.0, top_k};
+  wt.init(best, temperature, sm.power);
+  const Draw d{(double)u, (double)temperature, top_p, min_p > 0.f ? (double)fminf(min_p, 1.f) * (double)(1ull << kFraction) : 0.0, top_k};
   Beginning kept{-INFINITY, -1};
+  u64 unused;
   auto list_key = [&](int i, float l) {
     const int at = atomicAdd(&sm.n_list, 1);
     if (at < kListMax) sm.list_key[at] = (u64)order_key(l) << 32 | (unsigned)~i;
@@ -481,12 +501,22 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
         const float most = group_best[i * kWave];
         if (most > -INFINITY) atomicAdd(&sm.count[wt.bin(most)], 1);
       }
-      const int bin = find_bin<false>(sm, top_k, 0);
+      const int bin = find_bin<false>(sm, top_k, 0.0, unused);
       if (bin < kBins - 1) {
-        for (int i = 0; i < groups; ++i) {
-          if (wt.bin(group_best[i * kWave]) > bin) continue;
-          for (int k = i << shift; k < min((i + 1) << shift, run.n_units); ++k) {
-            const int at = run.index(k, 0);
+        // the groups that reach it, then their entries, a unit a thread: one trip to memory for all of them
+        int* reaching = (int*)sm.list_w;
+#pragma unroll 4
+        for (int i = 0; i < groups; ++i)
+          if (wt.bin(group_best[i * kWave]) <= bin) {
+            const int at = atomicAdd(&sm.n_groups, 1);
+            if (at < 2 * kListMax) reaching[at] = run.index(i << shift, 0);
+          }
+        __syncthreads();
+        const int n_groups = sm.n_groups;
+        if (n_groups <= 2 * kListMax) {
+          for (int g = tid; g < n_groups << shift; g += THREADS) {
+            const int at = reaching[g >> shift] + (g & ((1 << shift) - 1)) * (kWave * R::E);   // (the last group's may lie behind the row, or be the next wave's)
+            if ((g & ((1 << shift) - 1)) && at / (run.units * (kWave * R::E)) != reaching[g >> shift] / (run.units * (kWave * R::E))) continue;
             const u32x4 x = run.load_at(at);
 #pragma unroll
             for (int e = 0; e < R::E; ++e) {
@@ -494,7 +524,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
               if (wt.bin(l) <= bin) list_key(at + e, l);
             }
           }
-        }
+        } else if (tid == 0) sm.n_list = kListMax + 1;
         __syncthreads();
         const int n = sm.n_list;
         if (n <= kListMax) { draw_from_list(p, wt, d, n, sm); return; }
@@ -510,7 +540,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
     });
     limited = block_sum((u64)n_finite, sm) > (u64)top_k;
     if (limited) {
-      const int bin = find_bin<false>(sm, top_k, 0), before = sm.before_count;
+      const int bin = find_bin<false>(sm, top_k, 0.0, unused), before = sm.before_count;
       run.each([&](int i, float l) { if (l > -INFINITY && wt.bin(l) == bin) list_key(i, l); });
       __syncthreads();
       const int n = sm.n_list;
@@ -558,12 +588,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
   };
   bool summed = false;
   if (top_p < 1.f) {
-    u64 all = 0;
-    auto add_mass = [&](float l, int b) {
-      const u64 w = wt.of(l);
-      atomicAdd(&sm.mass[b], w);
-      all += w;
-    };
+    auto add_mass = [&](float l, int b) { atomicAdd(&sm.mass[b], wt.of(l)); };
     if (limited) run.each([&](int i, float l) {
       const int b = wt.bin(l);
       if (b < kBins - 1 && kept.has(i, l)) add_mass(l, b);
@@ -572,9 +597,8 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
       const int b = wt.bin(l);
       if (b < kBins - 1) add_mass(l, b);
     });
-    all = block_sum(all, sm);
-    const u64 need = min(max((u64)ceil((double)top_p * (double)all), (u64)1), all);
-    const int bin = find_bin<true>(sm, 0, need);
+    u64 need;
+    const int bin = find_bin<true>(sm, 0, (double)top_p, need);
     const u64 before = sm.before_mass;
     if (tid < WAVES) { sm.kept_mass[tid] = 0; sm.kept_count[tid] = 0; }
     run.each([&](int i, float l) {
@@ -652,7 +676,7 @@ __global__ __launch_bounds__(kWave * WAVES) void sample_kernel(SampleParams p) {
         sum += w[e];
       }
     }
-    const u64 upto = wave_scan(sum, lane);
+    const u64 upto = wave_scan(sum);
     __syncthreads();
     if (lane == kWave - 1) sm.wave_mass[wave] = upto;
     __syncthreads();

@@ -1,8 +1,7 @@
 """earn_sample against the definition in fp64 (oracle.sample_token): tokens, counts and log-probabilities.
 
-The library holds weights as multiples of 2^-44 of the best one's, each off by half of that and by a few 2^-53 of itself: a sum
-over n tokens is off by n 2^-45, and so is u or p times another one; with what 64-bit sums lose on either side that is less than
-n 2^-43.  The oracle tells how near to a border a row came; rows that come nearer than that are none of these (asserted).
+The library holds weights as multiples of 2^-44 of the best one's, each off by half of that and by 2^-46 of itself: a sum over n
+tokens is off by 3/2 n 2^-45, and so is u or p times another one; with what 64-bit sums lose on either side that is less than n 2^-43.  The oracle tells how near to a border a row came; rows that come nearer than that are none of these (asserted).
 Log-probabilities are fp32: half a step, and n 2^-43 from the sums (which are at least 1).
 """
 import numpy as np
