@@ -787,6 +787,7 @@ static int check_workspace(const char* who, size_t need, const void* workspace, 
     set_error("%s: workspace too small (%zu bytes given, %zu needed)", who, bytes, need);
     return EARN_ERR_WORKSPACE_TOO_SMALL;
   }
+  if (need > 0 && ((uintptr_t)workspace & 255)) { set_error("%s: the workspace must be 256-byte aligned", who); return EARN_ERR_INVALID_ARG; }
   return EARN_OK;
 }
 

@@ -96,14 +96,15 @@ __device__ __forceinline__ X wave_sum(X x) { return last_lane(wave_scan(x)); }
 // Weights of a row, as doubles times 2^kFraction.  exp((l - best) / T) = 2^(n / 512) exp(r ln 2 / 512) with n whole and |r| <= 1/2: a
 // table and the exponential series to the third power, whose next term is below 2^-46.
 struct Weights {
-  float best;         // the largest logit
-  float bins;         // bins per unit of logit
+  float best, half;   // the largest logit, half of it
+  float bins;         // bins per half a unit of logit
   double scale;       // kExpSteps log2(e) / T
   double c1, c2, c3;  // of the series, in scalar registers
   const double* power;   // 2^(i / kExpSteps), times 2^kFraction
   __device__ __forceinline__ void init(float best_, float temperature, const double* power_) {
     best = best_;
-    bins = fminf((float)kBinsPerUnit / temperature, 3e38f);
+    half = 0.5f * best_;
+    bins = fminf(2.f * (float)kBinsPerUnit / temperature, 3e38f);
     scale = kExpSteps * 1.4426950408889634074 / (double)temperature;
     power = power_;
     constexpr double c = 0.69314718055994530942 / kExpSteps;
@@ -121,8 +122,8 @@ struct Weights {
     return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull;
   }
   __device__ __forceinline__ u64 of(float l) const { return whole(real(l)); }
-  // monotone in l: rounding keeps the order of differences and products
-  __device__ __forceinline__ int bin(float l) const { return (int)fminf((best - l) * bins, (float)(kBins - 1)); }
+  // monotone in l: rounding keeps the order of differences and products.  (Halves: the difference of two logits may overflow.)
+  __device__ __forceinline__ int bin(float l) const { return (int)fminf(__builtin_fmaf(l, -0.5f, half) * bins, (float)(kBins - 1)); }
 };
 
 // 16 bytes at the alignment of an element

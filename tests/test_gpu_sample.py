@@ -164,6 +164,9 @@ def test_temperatures_and_logits_of_the_smallest_numbers():
     t = [1e-44, 3e-44, 1e-45, 1e-38, 1e38, 3e-37]
     for params in (dict(), dict(top_p=[0.8] * 6), dict(top_k=[4] * 6), dict(min_p=[0.1] * 6)):
         check(B, x, [0.0371, 0.4001, 0.9001, 0.3001, 0.6003, 0.9502], temperature=t, **params)
+    wide = torch.tensor([[3e38, -3e38, 1e38, -1e38, 0.0, 2e38]] * 4)          # differences beyond fp32
+    for params in (dict(), dict(top_p=[0.9] * 4), dict(top_k=[5] * 4, top_p=[0.95] * 4), dict(min_p=[0.02] * 4)):
+        check(B, wide, [0.05, 0.6, 0.9, 0.97], temperature=[1e38, 3e38, float("inf"), 7e37], **params)
     far = torch.tensor([[0.0, -1e-37, -2e-37, -1e-36, -5e-36, -1e38]] * 4)
     check(B, far, [0.1, 0.7, 0.95, 0.9999], temperature=[1e-37, 2e-37, 1e-38, 1e-45], top_p=[0.99] * 4)
 

@@ -48,6 +48,7 @@ def test_decode_refusals():
     assert more > need + 2 * 4 * 100000 * 4 > 0
     refused(call(bound=100000, ws_bytes=need - 1), B.EARN_ERR_WORKSPACE_TOO_SMALL)
     refused(call(bound=100000, ws=None), B.EARN_ERR_WORKSPACE_TOO_SMALL)
+    refused(call(bound=100000, ws=272), B.EARN_ERR_INVALID_ARG, "aligned")
     refused(call(bound=100000, w_out=FAKE, w_rows=10, ws_bytes=more - 1), B.EARN_ERR_WORKSPACE_TOO_SMALL)
     assert B.earn_decode_paged_workspace_bytes(_desc(d=96), 2, 100, False) == 0
     assert B.earn_decode_paged_workspace_bytes(_desc(hq=32, hkv=32), 64, 50, False) == 0
