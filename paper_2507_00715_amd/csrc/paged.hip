@@ -102,7 +102,7 @@ struct PagedParams {
   void* out;
   float* part_o; float* part_ml;         // [streams, hq, n_splits, d], [.., 2]
   float* scores;                         // [streams, hq, score_stride], base-2 exponents
-  int n_streams, hq, hkv, w_cap, max_len, n_splits, chunk, score_stride;
+  int n_streams, hq, hkv, w_cap, max_len, n_splits, chunk, score_stride, join_rows;
   float scale_log2;
   RopeTable rope;
   HeadMap heads;
@@ -625,7 +625,8 @@ __global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_m
 
 // Joins the splits' states.  Bound by its trips to memory, one behind the other: 128 splits of 12 heads with the weights of 65521 rows
 // 7 us (83 with a thread walking all splits).  Blocks x < Hq / Hkv of a (kv head, stream) give one query head's output each: 256 / (D / 8) lanes
-// share the splits, then meet in LDS.  The blocks behind them give 1024 rows' weights each.
+// share the splits, then meet in LDS.  The blocks behind them give
+// join_rows rows' weights each.
 constexpr int kJoinThreads = kPagedThreads, kMaxGroup = 128;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p) {
@@ -670,7 +671,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams p)
     Row8<T>::store((T*)p.out + ((long long)u * p.hq + head_of_slot(p.heads, c * gq + a)) * D + sb * 8, x);
     return;
   }
-  const int j0 = (int)(blockIdx.x - gq) * kWeightRows, j1 = min(min(n + 1, j0 + kWeightRows), p.w_cap);
+  const int j0 = (int)(blockIdx.x - gq) * p.join_rows, j1 = min(min(n + 1, j0 + p.join_rows), p.w_cap);
   if (j0 >= j1) return;
   __shared__ f32x2 state[kMaxGroup];
   add_weights<kJoinThreads>(p, u, c, n, j0, j1, state, [&]() {
@@ -1028,7 +1029,10 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
     {
-      const int row_blocks = w_out ? (int)(((long long)max_len + kWeightRows) / kWeightRows) : 0;
+      // rows of a block: 1024, more where the blocks are many (64 streams of up to 2080 rows, 32 heads: 16 -> 11 us)
+      const long long blocks = ((long long)max_len + kWeightRows) / kWeightRows, more = blocks * p.hkv * n_streams / 2048;
+      p.join_rows = kWeightRows * (int)(more < 1 ? 1 : more > 8 ? 8 : more);
+      const int row_blocks = w_out ? (int)(((long long)max_len + p.join_rows) / p.join_rows) : 0;
       hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(gq + row_blocks, p.hkv, n_streams), dim3(kJoinThreads), 0, stream, p);
     }
   });
