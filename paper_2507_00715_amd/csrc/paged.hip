@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restric
 // ------------------------------------------------------------------------------------------------------------------
 // The vector form (fp32): a row is spread over d / 8 lanes, a wave takes whole rows, every lane keeps softmax states of up to 8 query
 // heads over its share of them (larger groups: a workgroup each for 8 heads, which read the rows again).  Bound by HBM, with the
-// vector ALU near it: one stream of 32768 rows, 32 / 8 heads of 128 (268 MB), 64 us, 4.2 TB/s.
+// vector ALU near it: 8 streams of 16384 rows, 32 / 8 heads of 128 (1.07 GB), 207 us, 5.2 TB/s; one of 32768 (268 MB) 63.
 constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / kWave;
 constexpr int kPagedMaxChunk = 2048;   // rows of a split: its page numbers lie in LDS
 
@@ -169,7 +169,11 @@ __device__ __forceinline__ void finish_group(const PagedParams& p, long long fir
   }
 }
 
-template <typename T, int D, int GQ>
+// (fp32: two 16-byte halves)
+__device__ __forceinline__ Row8<float>::Raw streamed_row(const float* p) {
+  return Row8<float>::Raw{__builtin_nontemporal_load((const f32x4*)p), __builtin_nontemporal_load((const f32x4*)(p + 4))};
+}
+template <typename T, int D, int GQ, bool STREAMED>
 __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams p) {
   constexpr int LPK = D / 8, KPW = kWave / LPK;      // lanes per row, rows per wave instruction
   constexpr int NP = GQ >= 8 ? 2 : Row8<T>::kRowsInFlight;
@@ -266,8 +270,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
         const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
         if (page >= 0) {
           const long long from = row_offset<D>(p.pg, page, c, j - at * p.pg.page_size);
-          kr[i] = Row8<T>::load_raw(K + from);
-          vr[i] = Row8<T>::load_raw(V + from);
+          kr[i] = STREAMED ? streamed_row(K + from) : Row8<T>::load_raw(K + from);
+          vr[i] = STREAMED ? streamed_row(V + from) : Row8<T>::load_raw(V + from);
           there[i] = true;
         }
       }
@@ -715,7 +719,7 @@ __device__ __forceinline__ unsigned weight_key(float w) {
 // additions go to a few neighbouring bins, so that eight copies of it, a lane's by its number, take them in turn.  The rows
 // that agree in the first 11 bits are listed, a few hundred as a rule, and the other digits come from the list.  One workgroup
 // does all of it, so what bounds it is the vector instructions that every row takes in its few passes: the first histogram, the list,
-// two counts, the result.  8 x 8 heads of 32768 rows 29 us (one bit a pass, rows read again, 252), 64 x 2 of 1024-2048 rows 10 (25).
+// two counts, the result.  8 x 8 heads of 32768 rows 26 us (one bit a pass, rows read again, 252), 64 x 2 of 1024-2048 rows 10 (25).
 constexpr int kDigitBins = 2048, kDigitCopies = 8, kDigitList = 4096;
 struct SelectSmem {
   int bins[kDigitBins * kDigitCopies];
@@ -993,8 +997,8 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   const int rc = make_head_map(desc, &p.heads, "earn_decode_attn_paged");
   if (rc != EARN_OK) return rc;
   const bool mfma = desc->dtype == EARN_BF16;
-  // Values that the caches in front of the memory (256 MB) cannot hold until the next step are loaded without a place there: 16
-  // streams of 8192-32768 rows 237 -> 217 us; 256 streams of 100-500 rows, 63 MB, 19.2 -> 19.6.
+  // Rows that the caches in front of the memory (256 MB) cannot hold until the next step are loaded without a place there: 16 streams
+  // of 8192-32768 rows 237 -> 217 us; fp32, 8 of 16384, 217 -> 207; but 256 streams of 100-500 rows, 63 MB, 19.2 -> 19.6.
   const bool streamed = 2ll * n_streams * p.hkv * max_len * desc->head_dim * (mfma ? 2 : 4) > (256ll << 20);
   const int gq = p.hq / p.hkv, g = paged_heads(desc), parts = paged_parts(desc);
   // Eight waves share the rows of a stream that is not split, where no other workgroup would fill the CU: us, 32 streams of 256-528
@@ -1019,11 +1023,17 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
     else if (mfma && wide) mfma_launch(sixteen, std::false_type{}, eight);
     else if (mfma && g == 8) mfma_launch(eight, std::false_type{}, four);
     else if (mfma) mfma_launch(sixteen, std::false_type{}, four);
-    else if constexpr (sizeof(T) == 2) return;
-    else if (g == 1) hipLaunchKernelGGL((paged_decode_kernel<T, D, 1>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (g == 2) hipLaunchKernelGGL((paged_decode_kernel<T, D, 2>), grid, dim3(kPagedThreads), 0, stream, p);
-    else if (g == 4) hipLaunchKernelGGL((paged_decode_kernel<T, D, 4>), grid, dim3(kPagedThreads), 0, stream, p);
-    else hipLaunchKernelGGL((paged_decode_kernel<T, D, 8>), grid, dim3(kPagedThreads), 0, stream, p);
+    else if constexpr (sizeof(T) == 4) {
+      auto vector_launch = [&](auto heads) {
+        constexpr int G = decltype(heads)::value;
+        if (streamed) hipLaunchKernelGGL((paged_decode_kernel<T, D, G, true>), grid, dim3(kPagedThreads), 0, stream, p);
+        else hipLaunchKernelGGL((paged_decode_kernel<T, D, G, false>), grid, dim3(kPagedThreads), 0, stream, p);
+      };
+      if (g == 1) vector_launch(std::integral_constant<int, 1>{});
+      else if (g == 2) vector_launch(std::integral_constant<int, 2>{});
+      else if (g == 4) vector_launch(std::integral_constant<int, 4>{});
+      else vector_launch(eight);
+    }
   });
   if (p.part_o) for_type(desc, [&](auto t, auto d) {
     typedef decltype(t) T;
