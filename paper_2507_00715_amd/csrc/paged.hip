@@ -452,21 +452,22 @@ __global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_m
   const int n_blocks = (j_end - j_begin + BLK - 1) / BLK;
   // A block as it lies in memory: unit lane + 64 i of its rows, 16 bytes each.  Every unit is loaded, those of rows that are not
   // there from some row that is in the pool.  Returns which rows are there.
-  // Whole blocks over pages of a multiple of 16 rows: 16 rows lie in one page, one behind the other, and a wave looks their pages
-  // up once (one row at a time, a block took 590 vector instructions; 280 now).
+  // Whole blocks over pages of a multiple of 8 rows: 8 rows lie in one page, one behind the other, and a wave looks their pages up
+  // once (one row at a time, a block took 590 vector instructions; 280 now: 100 streams of 3000 rows, 32 heads over 8, pages of 8,
+  // 132 us for 155).
   constexpr int RPI = kWave / UPR;                    // rows of 64 units
-  const bool by_sixteen = p.pg.page_size % 16 == 0;
-  auto load_block = [&](u32x4 (&x)[NV], const __bf16* pool, int blk) {
+  const bool by_eight = p.pg.page_size % 8 == 0;
+  auto load_block = [&](u32x4 (&x)[NV], const __bf16* pool, int blk) __attribute__((always_inline)) {
     const int j0 = j_begin + blk * BLK;
     unsigned have = 0;                                // bit i: row i of the block has a place in the pool
-    if (by_sixteen && j0 + BLK <= min(n, j_end)) {
+    if (by_eight && j0 + BLK <= min(n, j_end)) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int j = j0 + 16 * t, at = (int)p.pg.by_page.div((unsigned)j), page = __builtin_amdgcn_readfirstlane(pages[at - page0]);
+      for (int t = 0; t < 4; ++t) {
+        const int j = j0 + 8 * t, at = (int)p.pg.by_page.div((unsigned)j), page = __builtin_amdgcn_readfirstlane(pages[at - page0]);
         const u32x4* rows = (const u32x4*)(pool + row_offset<D>(p.pg, max(page, 0), c, j - at * p.pg.page_size));
-        have |= page >= 0 ? 0xffffu << (16 * t) : 0u;
+        have |= page >= 0 ? 0xffu << (8 * t) : 0u;
 #pragma unroll
-        for (int i = 0; i < NV / 2; ++i) x[t * (NV / 2) + i] = STREAMED ? __builtin_nontemporal_load(rows + lane + kWave * i) : rows[lane + kWave * i];
+        for (int i = 0; i < NV / 4; ++i) x[t * (NV / 4) + i] = STREAMED ? __builtin_nontemporal_load(rows + lane + kWave * i) : rows[lane + kWave * i];
       }
       return have;
     }

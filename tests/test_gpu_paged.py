@@ -221,6 +221,21 @@ def test_rows_without_a_page_weigh_nothing(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [8, 24])
+def test_holes_of_eight_rows_within_a_block(dtype, d, page):
+    """Pages missing inside the 32 rows that are read together, at each place of them."""
+    B = _B()
+    case = Case(dtype, 4, 2, d, page, [96, 100, 32, 192])
+    case.table[0, [0, 2]] = -1
+    case.table[1, [1, 3]] = [case.n_pages, -7]
+    case.table[2, 1] = -1
+    case.table[3, 1:7] = -1
+    out, w_out = case.run(B, True)
+    case.check(out, w_out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_streams_share_pages(dtype):
     B = _B()
     case = Case(dtype, 8, 2, 64, 16, [100, 90, 64])
