@@ -438,7 +438,8 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  *               row's sum starts here); rows behind n are left as they are, rows from weight_rows on have no sum
  *   weights_in  the same layout, or NULL (zeros); may be weights_out itself
  *   out         [n_streams, Hq, d]
- *   workspace   at least earn_decode_paged_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0
+ *   workspace   at least earn_decode_paged_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.  The size never
+ *               falls as n_streams or max_cache_len grow, or where weights are asked for: one for the largest call serves all
  * Errors: as earn_decode_attn; more than 128 query heads per kv head -> UNSUPPORTED.  Long caches are split over workgroups and joined in
  * a second launch.
  *

@@ -933,6 +933,7 @@ int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v,
 }
 
 struct PagedPlan { int n_splits, chunk, score_stride; size_t part_o, part_ml, scores; };
+constexpr int kWholeRows = 640, kMinChunk = 256, kMostChunk = 1088;
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // query heads that a workgroup serves, and the workgroups of a group of heads
 static int paged_heads(const earn_attn_desc* desc) {
@@ -944,20 +945,21 @@ static int paged_parts(const earn_attn_desc* desc) {
   const int gq = desc->n_q_heads / desc->n_kv_heads, heads = paged_heads(desc);
   return (gq + heads - 1) / heads;
 }
+static int wanted_workgroups(const earn_attn_desc* desc) { return desc->dtype == EARN_F32 ? 512 : 256; }
 static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
   PagedPlan pl{};
   const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
-  // Rows of a split: what leaves a workgroup per CU (fp32, whose workgroups are lighter: two), from 256, below
-  // which a workgroup's start costs more than its rows, to 1088, above which the long streams' last splits run on their own.  Up to
-  // 640 rows nothing is split: the joining launch costs as much as it saves.  us, 256 / 512 / 1024 / 2048 rows: 8 streams of 2000 rows, 32
+  // Rows of a split: what leaves a workgroup per CU (fp32, whose workgroups are lighter: two), from kMinChunk, below
+  // which a workgroup's start costs more than its rows, to kMostChunk, above which the long streams' last splits run on their own.  Up to
+  // kWholeRows rows nothing is split: the joining launch costs as much as it saves.  us, 256 / 512 / 1024 / 2048 rows: 8 streams of 2000 rows, 32
   // / 32 heads 65 / 61 / 60 / 58; 4 of 8192, 32 / 8 heads 37 / 35 / 29 / 36; one of 4096 14 / 16 / 22 / 34; 16 of 8192-32768 270 / 228 / 214
   // / 212; one of 65521, 12 / 2 heads 26 / 24 / 27 / 39; one of 32768, fp32 74 / 64 / 70 / 118; 32 of 256-528, 14 / 2 heads of 64 12.2 / 14.4 /
   // 11.5 whole; 256 of 100-500, 12 / 2 heads 29 / 20 whole.
   const int forced = tuning(kTunePagedChunk, 0);
-  long long chunk = rows * pairs / (desc->dtype == EARN_F32 ? 512 : 256);
-  if (chunk < 256) chunk = 256;
-  if (chunk > 1088) chunk = 1088;
-  if (rows <= 640) chunk = rows;
+  long long chunk = rows * pairs / wanted_workgroups(desc);
+  if (chunk < kMinChunk) chunk = kMinChunk;
+  if (chunk > kMostChunk) chunk = kMostChunk;
+  if (rows <= kWholeRows) chunk = rows;
   if (forced > 0) chunk = forced < kPagedMaxChunk ? forced : kPagedMaxChunk;
   if (chunk > rows) chunk = rows;
   if (chunk < rows / 65535 + 1) chunk = rows / 65535 + 1;   // a grid dimension
@@ -973,9 +975,24 @@ static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_l
   if (weights) pl.scores = up256(heads * pl.score_stride * 4);
   return pl;
 }
+// What any call of at most n_streams streams and max_len rows takes by plan_paged: splits get longer, and fewer, as either grows, but
+// a workspace sized for the largest call has to serve the smaller ones.  With n streams of hkv heads, r rows, c rows a split and W
+// workgroups wanted:  c >= kMinChunk, so n splits <= n ceil(r / kMinChunk);  and either c = kMostChunk, so n splits <= n ceil(r /
+// kMostChunk), or r n hkv / W < c + 1 (its division leaves a rest), so n splits < n (r / c + 1) < W (kMinChunk + 1) / (kMinChunk hkv) + n.
 size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
-  const PagedPlan pl = plan_paged(desc, n_streams, max_len, weights);
-  return pl.part_o + pl.part_ml + pl.scores;
+  const long long rows = (long long)max_len + 1, n = n_streams;
+  auto of = [](long long r, long long c) { return (r + c - 1) / c; };
+  const int forced = tuning(kTunePagedChunk, 0);
+  long long splits = n;                          // of all streams
+  if (forced > 0) splits = n * min(of(rows, (min(forced, kPagedMaxChunk) + 63) / 64 * 64), 65535ll);
+  else if (rows > kWholeRows)
+    splits = min(n * of(rows, kMinChunk),
+                 max(n * of(rows, kMostChunk), (long long)wanted_workgroups(desc) * (kMinChunk + 1) / (kMinChunk * desc->n_kv_heads) + n));
+  const size_t heads = (size_t)n * desc->n_q_heads;
+  size_t bytes = weights ? up256(heads * ((rows + 31) / 32 * 32) * 4) : 0;
+  if (splits > n || (weights && paged_parts(desc) > 1))
+    bytes += up256((size_t)splits * desc->n_q_heads * desc->head_dim * 4) + up256((size_t)splits * desc->n_q_heads * 8);
+  return bytes;
 }
 
 int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new, const int32_t* q_pos,
