@@ -86,11 +86,11 @@ int launch_attn_backward(const earn_attn_desc* desc, const void* q, const void* 
 int launch_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu, const int32_t* start, int batch,
                        int total, void* k_pages, void* v_pages, const int32_t* table, int max_pages, int n_pages, int page_size,
                        hipStream_t stream);
-size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights);
+size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights, int forced);
 int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new, const int32_t* q_pos,
                         void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len, int n_streams, int max_pages,
                         int n_pages, int page_size, int max_len, const float* w_in, float* w_out, int w_cap, void* out,
-                        void* workspace, hipStream_t stream);
+                        void* workspace, int forced, hipStream_t stream);
 int launch_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len,
                        int n_streams, int max_pages, int n_pages, int page_size, int max_len, const float* w_in, int w_cap, int budget,
                        int first, int last, const int32_t* new_table, int new_pages, int32_t* kept, int32_t* len_out, float* w_out,
@@ -823,7 +823,7 @@ size_t earn_decode_paged_workspace_bytes(const earn_attn_desc* desc, int32_t n_s
   if (check_paged_desc(desc, n_streams, "earn_decode_paged_workspace_bytes") != EARN_OK || n_streams <= 0 || max_cache_len < 0 ||
       max_cache_len > EARN_MAX_CACHE_LEN)
     return 0;
-  return decode_paged_workspace_bytes(desc, n_streams, max_cache_len, have_weights != 0);
+  return decode_paged_workspace_bytes(desc, n_streams, max_cache_len, have_weights != 0, tuning(kTunePagedChunk, 0));
 }
 
 int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new,
@@ -844,11 +844,12 @@ int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void
   if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) { set_error("%s: q, k_new, v_new and out must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
   if (weights_in && !weights_out) { set_error("%s: weights_in without weights_out", who); return EARN_ERR_INVALID_ARG; }
   if (weights_out && weight_rows <= 0) { set_error("%s: weight_rows (%d) must be positive", who, weight_rows); return EARN_ERR_INVALID_ARG; }
-  const size_t need = decode_paged_workspace_bytes(desc, n_streams, max_cache_len, weights_out != nullptr);
+  const int forced = tuning(kTunePagedChunk, 0);   // read once: the size checked is that of the launch, whoever sets it meanwhile
+  const size_t need = decode_paged_workspace_bytes(desc, n_streams, max_cache_len, weights_out != nullptr, forced);
   if ((rc = check_workspace(who, need, workspace, workspace_bytes)) != EARN_OK) return rc;
   if (g_validate.load(std::memory_order_relaxed) && (rc = guarded(who, [&] { return validate_decode_paged(who, q_pos, cache_len, page_table, n_streams, max_cache_len, max_pages, n_pages, page_size, stream); })) != EARN_OK) return rc;
   return launch_decode_paged(desc, q, k_new, v_new, q_pos, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages,
-                             page_size, max_cache_len, weights_in, weights_out, weight_rows, out, workspace, (hipStream_t)stream);
+                             page_size, max_cache_len, weights_in, weights_out, weight_rows, out, workspace, forced, (hipStream_t)stream);
 }
 
 size_t earn_cache_evict_workspace_bytes(const earn_attn_desc* desc, int32_t n_streams, int32_t max_cache_len, int32_t budget) {

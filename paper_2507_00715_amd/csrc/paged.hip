@@ -946,7 +946,8 @@ static int paged_parts(const earn_attn_desc* desc) {
   return (gq + heads - 1) / heads;
 }
 static int wanted_workgroups(const earn_attn_desc* desc) { return desc->dtype == EARN_F32 ? 512 : 256; }
-static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
+// `forced`: the setting of "paged_chunk", 0 for none; a call reads it once, for the size that it asks for and for what it launches
+static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_len, bool weights, int forced) {
   PagedPlan pl{};
   const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
   // Rows of a split: what leaves a workgroup per CU (fp32, whose workgroups are lighter: two), from kMinChunk, below
@@ -955,7 +956,6 @@ static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_l
   // / 32 heads 65 / 61 / 60 / 58; 4 of 8192, 32 / 8 heads 37 / 35 / 29 / 36; one of 4096 14 / 16 / 22 / 34; 16 of 8192-32768 270 / 228 / 214
   // / 212; one of 65521, 12 / 2 heads 26 / 24 / 27 / 39; one of 32768, fp32 74 / 64 / 70 / 118; 32 of 256-528, 14 / 2 heads of 64 12.2 / 14.4 /
   // 11.5 whole; 256 of 100-500, 12 / 2 heads 29 / 20 whole.
-  const int forced = tuning(kTunePagedChunk, 0);
   long long chunk = rows * pairs / wanted_workgroups(desc);
   if (chunk < kMinChunk) chunk = kMinChunk;
   if (chunk > kMostChunk) chunk = kMostChunk;
@@ -979,10 +979,9 @@ static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_l
 // a workspace sized for the largest call has to serve the smaller ones.  With n streams of hkv heads, r rows, c rows a split and W
 // workgroups wanted:  c >= kMinChunk, so n splits <= n ceil(r / kMinChunk);  and either c = kMostChunk, so n splits <= n ceil(r /
 // kMostChunk), or r n hkv / W < c + 1 (its division leaves a rest), so n splits < n (r / c + 1) < W (kMinChunk + 1) / (kMinChunk hkv) + n.
-size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights) {
+size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, int max_len, bool weights, int forced) {
   const long long rows = (long long)max_len + 1, n = n_streams;
   auto of = [](long long r, long long c) { return (r + c - 1) / c; };
-  const int forced = tuning(kTunePagedChunk, 0);
   long long splits = n;                          // of all streams
   if (forced > 0) splits = n * min(of(rows, (min(forced, kPagedMaxChunk) + 63) / 64 * 64), 65535ll);
   else if (rows > kWholeRows)
@@ -998,8 +997,8 @@ size_t decode_paged_workspace_bytes(const earn_attn_desc* desc, int n_streams, i
 int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k_new, const void* v_new, const int32_t* q_pos,
                         void* k_pages, void* v_pages, const int32_t* table, const int32_t* cache_len, int n_streams, int max_pages,
                         int n_pages, int page_size, int max_len, const float* w_in, float* w_out, int w_cap, void* out,
-                        void* workspace, hipStream_t stream) {
-  const PagedPlan pl = plan_paged(desc, n_streams, max_len, w_out != nullptr);
+                        void* workspace, int forced, hipStream_t stream) {
+  const PagedPlan pl = plan_paged(desc, n_streams, max_len, w_out != nullptr, forced);
   PagedParams p;
   p.pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
   p.q = q; p.k_new = k_new; p.v_new = v_new; p.q_pos = q_pos; p.cache_len = cache_len;
