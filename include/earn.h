@@ -436,6 +436,8 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  *   weights_out [n_streams, Hkv, weight_rows] fp32 or NULL: running sums of the softmax weights, per kv head over its query heads:
  *               weights_out[u][c][r] = weights_in[u][c][r] + sum_a p_a(r)   for r < n, and without weights_in for r = n (a new
  *               row's sum starts here); rows behind n are left as they are, rows from weight_rows on have no sum
+ *               (where a head's softmax is NaN, as when a score is +inf or all are -inf, so is what it adds to every row that has a
+ *               place; rows without one get nothing)
  *   weights_in  the same layout, or NULL (zeros); may be weights_out itself
  *   out         [n_streams, Hq, d]
  *   workspace   at least earn_decode_paged_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.  The size never

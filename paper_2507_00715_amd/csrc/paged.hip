@@ -95,13 +95,17 @@ __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restric
 constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / kWave;
 constexpr int kPagedMaxChunk = 2048;   // rows of a split: its page numbers lie in LDS
 
+// What stands among the scores for a row that is not there, and weighs 0 whatever the others are.  A signalling NaN, which no sum or product
+// gives: a score that is -inf, or NaN, is a row's own.
+constexpr unsigned kNoRow = 0x7fa00000u;
+
 struct PagedParams {
   Pages pg;
   const void* q; const void* k_new; const void* v_new; const int32_t* q_pos; const int32_t* cache_len;
   const float* w_in; float* w_out;       // [streams, hkv, w_cap]
   void* out;
   float* part_o; float* part_ml;         // [streams, hq, n_splits, d], [.., 2]
-  float* scores;                         // [streams, hq, score_stride], base-2 exponents
+  float* scores;                         // [streams, hq, score_stride], base-2 exponents; kNoRow: a row without a page
   int n_streams, hq, hkv, w_cap, max_len, n_splits, chunk, score_stride, join_rows;
   float scale_log2;
   RopeTable rope;
@@ -120,17 +124,18 @@ constexpr int kWeightRows = 4 * kPagedThreads;   // of one round of kPagedThread
 template <int THREADS, typename States>
 __device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, int n, int j0, int j1, const f32x2* state, States states) {
   const int gq = p.hq / p.hkv, tid = threadIdx.x;
-  const float* scores = p.scores + ((long long)u * p.hq + c * gq) * p.score_stride;
+  const unsigned* scores = (const unsigned*)p.scores + ((long long)u * p.hq + c * gq) * p.score_stride;
   const long long to = ((long long)u * p.hkv + c) * p.w_cap;
   bool first = true;
   for (int jb = j0; jb < j1; jb += 4 * THREADS) {
-    float w[4], old[4], s[4];
+    float w[4], old[4];
+    unsigned s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int j = jb + i * THREADS + tid;
       w[i] = 0.f;
       old[i] = j < j1 && j < n && p.w_in ? p.w_in[to + j] : 0.f;
-      s[i] = j < j1 ? scores[j] : -INFINITY;
+      s[i] = j < j1 ? scores[j] : kNoRow;
     }
     if (first) { states(); first = false; }
     for (int a = 0; a < gq; ++a) {
@@ -138,12 +143,12 @@ __device__ __forceinline__ void add_weights(const PagedParams& p, int u, int c, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int j = jb + i * THREADS + tid;
-          s[i] = j < j1 ? scores[(long long)a * p.score_stride + j] : -INFINITY;
+          s[i] = j < j1 ? scores[(long long)a * p.score_stride + j] : kNoRow;
         }
       }
       const f32x2 st = state[a];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] += s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[i] - st[0]) * st[1];
+      for (int i = 0; i < 4; ++i) w[i] += s[i] == kNoRow ? 0.f : __builtin_amdgcn_exp2f(__uint_as_float(s[i]) - st[0]) * st[1];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
         d = group_sum<LPK>(d);
         sc[i][a] = there[i] ? d : -INFINITY;
         if (p.scores && sub == 0 && a < na && j < j_end)
-          p.scores[((long long)u * p.hq + c * gq + a0 + a) * p.score_stride + j] = sc[i][a];
+          ((unsigned*)p.scores)[((long long)u * p.hq + c * gq + a0 + a) * p.score_stride + j] = there[i] ? __float_as_uint(d) : kNoRow;
       }
     }
 #pragma unroll
@@ -560,16 +565,23 @@ __global__ __launch_bounds__(kWave * WAVES, D == 64 ? 3 : 2) void paged_decode_m
         if (j_new < BLK && lane < UPR) *(u32x4*)(smv + j_new * D + ((lane ^ short_v_swz<D>(j_new)) << 3)) = newest;
       }
       if (more) load_block(vr, (const __bf16*)p.pg.v, blk + WAVES);
+      if (scores && r16 < na) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          u32x4 x = __builtin_bit_cast(u32x4, sc[t]);
+          if (mask != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = mask >> (16 * t + 4 * quad + i) & 1 ? x[i] : kNoRow;
+          }
+          *(u32x4*)(scores + j0 + 16 * t + 4 * quad) = x;
+        }
+      }
       if (mask != 0xffffffffu) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (!(mask >> (16 * t + 4 * quad + i) & 1)) sc[t][i] = -INFINITY;
-      }
-      if (scores && r16 < na) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) *(f32x4*)(scores + j0 + 16 * t + 4 * quad) = sc[t];
       }
       u32x4 pw[3];
       const float alpha = short_softmax(sc, mrow, lrow, pw);

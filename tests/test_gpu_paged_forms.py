@@ -59,3 +59,37 @@ def test_a_setting_that_changes_during_a_call_does_not_outgrow_its_workspace(dty
         assert (whole[need:] == 0x5A).all()
     finally:
         B.earn_set_tuning("paged_chunk", 0)
+
+
+@pytest.mark.parametrize("n", [90, 1500], ids=["whole", "split"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_weights_follow_a_softmax_that_is_nan(dtype, n):
+    """Where all scores are -inf, or one is +inf or NaN, every weight of that softmax is NaN, that of a row of score -inf too; rows
+    without a page weigh 0 all the same, and another kv head's sums are untouched by it."""
+    B = _B()
+    page, inf = 16, float("inf")
+    case = Case(dtype, 2, 2, 64, page, [n] * 4)
+    case.table[:, 2] = -1                                   # rows 32 .. 47 are not there
+    desc = B.make_desc(dtype, 2, 2, 64, rope_base=0.0)
+    case.q[:, 0] = case.q[:, 0].abs() + 0.5
+    lowest = torch.finfo(dtype).min
+    at = lambda u, r: (int(case.table[u, r // page]), 0, r % page)
+    for r in [r for r in range(n) if r // page != 2]:
+        case.kp[at(0, r)] = lowest                          # products of 64 of them overflow
+        if r < 20:
+            case.kp[at(1, r)] = lowest
+            case.kp[at(2, r)] = lowest
+            case.kp[at(3, r)] = lowest
+    case.kn[0, 0] = lowest
+    case.kp[at(1, n - 5)] = inf
+    case.kp[at(2, 60)] = float("nan")
+    out, w_out = case.run(B, True, desc=desc)
+    there = torch.ones(n + 1, dtype=torch.bool)
+    there[32:48] = False
+    for u in range(3):
+        assert torch.isnan(out[u, 0].float()).all(), u
+        assert torch.equal(torch.isnan(w_out[u, 0, :n + 1].cpu()), there), u
+        assert torch.equal(w_out[u, 0, 32:48].cpu(), case.w_in[u, 0, 32:48]), u
+    assert torch.isfinite(out[3].float()).all() and torch.isfinite(w_out[3]).all()
+    assert torch.equal(w_out[3, 0, :20].cpu(), case.w_in[3, 0, :20])       # -inf among finite scores: nothing
+    assert torch.isfinite(out[:, 1].float()).all() and torch.isfinite(w_out[:, 1]).all()
