@@ -430,7 +430,8 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  *   q' = RoPE(q_u, q_pos[u]);  k' = RoPE(k_new_u, q_pos[u]), rounded to the cache's type;  row n of the stream := (k', v_new_u)
  *   out_u = softmax over rows 0 .. n of (q' . key * scale), times values
  * A position is not a row number: caches that rows were evicted from go on at their streams' own positions.  A new row without
- * a place (no page, or n at the table's end) is attended but not stored.
+ * a place (no page, or n at the table's end) is attended but not stored; it is not there at the next step, and not counted in
+ * cache_len by a caller who evicts later.  (earn_set_validation(1) refuses such a step.)
  *   q           [n_streams, Hq, d]                     k_new, v_new  [n_streams, Hkv, d], k_new not yet rotated
  *   q_pos, cache_len  [n_streams] int32, device        max_cache_len  upper bound on cache_len
  *   weights_out [n_streams, Hkv, weight_rows] fp32 or NULL: running sums of the softmax weights, per kv head over its query heads:
@@ -450,6 +451,8 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  * as less than anything; n = cache_len[u]).  The kept rows move in their order to rows 0, 1, ... of the pages that new_table
  * names; a stream of at most `budget` rows moves whole.  The old pages and weights are only read: the caller goes on with
  * new_table, len_out and weights_out and may then use the old pages for other streams.
+ * PRECONDITION (earn_set_validation(1) checks it): every row below cache_len has a page.  A row without one is kept or not by its
+ * weight like the others and arrives as a row of zeros that HAS a place: later steps, which did not attend to it before, do.
  *   weights     [n_streams, Hkv, weight_rows] fp32 (weights_out of the decode steps); cache_len <= weight_rows
  *   new_table   [n_streams, new_max_pages] int32, device: pages of the same pools that no stream of the call reads from, each
  *               named once; new_max_pages * page_size >= budget

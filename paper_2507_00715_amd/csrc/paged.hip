@@ -900,7 +900,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   const int at = (int)p.pg.by_page.div((unsigned)i), page = p.new_table[(long long)u * p.new_pages + at];
   if ((unsigned)page >= (unsigned)p.pg.n_pages) return;
   const long long to = row_offset<D>(p.pg, page, c, i - at * p.pg.page_size) * (long long)sizeof(T) / 16 + unit;
-  u32x4 k = {0u, 0u, 0u, 0u}, v = k;             // a row without a page: zeros
+  u32x4 k = {0u, 0u, 0u, 0u}, v = k;             // a row without a page, which no caller hands over: zeros, not what the new page held
   if (old >= 0) {
     const long long from = row_offset<D>(p.pg, old, c, in_old) * (long long)sizeof(T) / 16 + unit;
     k = __builtin_nontemporal_load((const u32x4*)p.pg.k + from);

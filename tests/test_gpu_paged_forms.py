@@ -93,3 +93,47 @@ def test_weights_follow_a_softmax_that_is_nan(dtype, n):
     assert torch.isfinite(out[3].float()).all() and torch.isfinite(w_out[3]).all()
     assert torch.equal(w_out[3, 0, :20].cpu(), case.w_in[3, 0, :20])       # -inf among finite scores: nothing
     assert torch.isfinite(out[:, 1].float()).all() and torch.isfinite(w_out[:, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("budget", [40, 100])
+def test_a_row_without_a_page_is_a_row_of_zeros_after_eviction(dtype, budget):
+    """Eviction's precondition is that every row has a page.  Where one has none, it comes out as documented: zeros that the next step
+    attends to (cut down to the budget, and moved whole), and the validation mode refuses the call."""
+    B = _B()
+    page, n = 16, 90
+    case = Case(dtype, 4, 2, 64, page, [n])
+    case.table[0, 2] = -1                                   # rows 32 .. 47
+    desc = B.make_desc(dtype, 4, 2, 64)
+    kp, vp = case.kp.to(DEV), case.vp.to(DEV)
+    per = -(-(budget + 1) // page)
+    m, base = min(n, budget), kp.shape[0]
+    grow = lambda x: torch.cat([x, torch.full((per, 2, page, 64), float("nan"), dtype=dtype, device=DEV)])
+    kp, vp = grow(kp), grow(vp)
+    fresh = i32([list(range(base, base + per))])
+    kept, length = torch.empty(1, 2, budget, dtype=torch.int32, device=DEV), i32([0])
+    w = case.w_in.to(DEV)
+    w[:, :, 30:50] += 1.0                                   # the rows that are not there are among the largest
+    old = B.earn_set_validation(True)
+    try:
+        with pytest.raises(B.EarnError) as e:
+            B.earn_cache_evict(desc, kp, vp, i32(case.table), i32([n]), n, w, budget, 2, 3, fresh, kept, length)
+        assert e.value.code == B.EARN_ERR_INVALID_ARG and "page_table[0][2] = -1" in str(e.value)
+    finally:
+        B.earn_set_validation(old)
+    B.earn_cache_evict(desc, kp, vp, i32(case.table), i32([n]), n, w, budget, 2, 3, fresh, kept, length)
+    torch.cuda.synchronize()
+    assert length.tolist() == [m] and set(range(32, 48)) <= set(kept[0, 0].tolist()) & set(kept[0, 1].tolist())
+    after = Case(dtype, 4, 2, 64, page, [m])
+    after.q, after.kn, after.vn = case.q, case.kn, case.vn
+    after.n_pages = per
+    after.table = torch.arange(per, dtype=torch.int32).numpy()[None]
+    after.kp, after.vp = kp[base:].cpu(), vp[base:].cpu()
+    for c in range(2):
+        for i, r in enumerate(kept[0, c].tolist()[:m]):
+            got = after.kp[i // page, c, i % page]
+            assert torch.equal(got, torch.zeros(64, dtype=dtype) if 32 <= r < 48 else case.kp[int(case.table[0, r // page]), c, r % page])
+    out, w_out = after.run(B, True)
+    after.kp, after.vp = after.kp.nan_to_num(0.0), after.vp.nan_to_num(0.0)      # behind the last row
+    after.g_kp, after.g_vp = after.g_kp.nan_to_num(0.0), after.g_vp.nan_to_num(0.0)
+    after.check(out, w_out)
