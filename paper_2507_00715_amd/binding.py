@@ -485,21 +485,26 @@ def _current() -> int:
 def _pool(k_pages, v_pages, desc: AttnDesc):
     """(n_pages, page_size) of [n_pages, Hkv, page_size, d] pools."""
     n_pages, heads, page_size, d = k_pages.shape
-    assert heads == desc.n_kv_heads and d == desc.head_dim, "the pools [n_pages, Hkv, page_size, d] have other heads than the description"
-    assert v_pages.shape == k_pages.shape and v_pages.dtype is k_pages.dtype
-    assert k_pages.dtype is (torch.float32 if desc.dtype == EARN_F32 else torch.bfloat16), "the pools have another type than the description"
+    if heads != desc.n_kv_heads or d != desc.head_dim:
+        raise AssertionError("the pools [n_pages, Hkv, page_size, d] have other heads than the description")
+    if v_pages.shape != k_pages.shape or v_pages.dtype is not k_pages.dtype:
+        raise AssertionError("the pools of keys and of values differ in shape or type")
+    if k_pages.dtype is not (torch.float32 if desc.dtype == EARN_F32 else torch.bfloat16):
+        raise AssertionError("the pools have another type than the description")
     return n_pages, page_size
 
 
 def _i32(*tensors) -> None:
     """The library is told no types of index arrays: they have to be what the header says."""
     for t in tensors:
-        assert t is None or t.dtype is torch.int32, "index arrays are int32"
+        if t is not None and t.dtype is not torch.int32:
+            raise AssertionError("index arrays are int32")
 
 
 def _f32(*tensors) -> None:
     for t in tensors:
-        assert t is None or t.dtype is torch.float32, "weights and parameters are fp32"
+        if t is not None and t.dtype is not torch.float32:
+            raise AssertionError("weights and parameters are fp32")
 
 
 def earn_cache_store(desc: AttnDesc, k, v, cu_seqlens, start, k_pages, v_pages, page_table) -> None:
@@ -508,8 +513,10 @@ def earn_cache_store(desc: AttnDesc, k, v, cu_seqlens, start, k_pages, v_pages, 
     _i32(cu_seqlens, start, page_table)
     batch, max_pages = page_table.shape
     total, heads, d = k.shape
-    assert heads == desc.n_kv_heads and d == desc.head_dim and v.shape == k.shape and k.dtype is v.dtype is k_pages.dtype
-    assert cu_seqlens.numel() == batch + 1 and (start is None or start.numel() == batch)
+    if not (heads == desc.n_kv_heads and d == desc.head_dim and v.shape == k.shape and k.dtype is v.dtype is k_pages.dtype):
+        raise AssertionError("k and v are [total_tokens, Hkv, d] of the pools' type")
+    if cu_seqlens.numel() != batch + 1 or (start is not None and start.numel() != batch):
+        raise AssertionError("cu_seqlens has batch + 1 entries, start and page_table batch")
     a = _on(_current(), k, v, cu_seqlens, start, k_pages, v_pages, page_table)
     _check(lib().earn_cache_store(ctypes.byref(desc), a[0], a[1], a[2], a[3], batch, total, a[4], a[5], a[6], max_pages, n_pages,
                                   page_size, _stream()))
@@ -525,14 +532,18 @@ def _decode_paged_args(desc: AttnDesc, q, k_new, v_new, q_pos, k_pages, v_pages,
     _i32(q_pos, page_table, cache_len)
     n, max_pages = page_table.shape
     hkv, d = desc.n_kv_heads, desc.head_dim
-    assert q.shape == out.shape == (n, desc.n_q_heads, d) and k_new.shape == v_new.shape == (n, hkv, d)
-    assert q.dtype is k_new.dtype is v_new.dtype is out.dtype is k_pages.dtype
-    assert q_pos.numel() == cache_len.numel() == n
+    if not (q.shape == out.shape == (n, desc.n_q_heads, d) and k_new.shape == v_new.shape == (n, hkv, d)):
+        raise AssertionError("q and out are [n_streams, Hq, d], k_new and v_new [n_streams, Hkv, d]")
+    if not q.dtype is k_new.dtype is v_new.dtype is out.dtype is k_pages.dtype:
+        raise AssertionError("q, k_new, v_new and out are of the pools' type")
+    if not q_pos.numel() == cache_len.numel() == n:
+        raise AssertionError("q_pos and cache_len have one entry a stream")
     rows = 0
     if weights_out is not None:
         _f32(weights_in, weights_out)
         rows = weights_out.shape[-1]
-        assert weights_out.shape == (n, hkv, rows) and (weights_in is None or weights_in.shape == weights_out.shape)
+        if weights_out.shape != (n, hkv, rows) or (weights_in is not None and weights_in.shape != weights_out.shape):
+            raise AssertionError("weights are [n_streams, Hkv, weight_rows], in and out alike")
     if workspace is None:   # one-off calls; loops pass a buffer of their own
         need = earn_decode_paged_workspace_bytes(desc, n, max_cache_len, weights_out is not None)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
@@ -568,8 +579,12 @@ def earn_cache_evict(desc: AttnDesc, k_pages, v_pages, page_table, cache_len, ma
     hkv = desc.n_kv_heads
     _i32(page_table, cache_len, new_table, kept_out, len_out)
     _f32(weights, weights_out)
-    assert cache_len.numel() == len_out.numel() == n and new_table.shape[0] == n and kept_out.shape == (n, hkv, budget)
-    assert weights.shape[:2] == (n, hkv) and (weights_out is None or weights_out.shape[:2] == (n, hkv))
+    if not (cache_len.numel() == len_out.numel() == n and new_table.dim() == 2 and new_table.shape[0] == n and
+            kept_out.shape == (n, hkv, budget)):
+        raise AssertionError("one length and one row of each table a stream, kept_out [n_streams, Hkv, budget]")
+    for w in (weights, weights_out):
+        if w is not None and (w.dim() != 3 or w.shape[:2] != (n, hkv)):
+            raise AssertionError("weights are [n_streams, Hkv, weight_rows]")
     if workspace is None:
         need = earn_cache_evict_workspace_bytes(desc, n, max_cache_len, budget)
         workspace = torch.empty(need, dtype=torch.uint8, device=k_pages.device) if need else None
@@ -588,12 +603,14 @@ def earn_sample(logits, uniform, token_out, temperature=None, top_k=None, top_p=
     """logits [rows, vocab], fp32 or bf16, rows at any distance (a slice of wider rows is taken as it is)."""
     code = EARN_F32 if logits.dtype is torch.float32 else EARN_BF16 if logits.dtype is torch.bfloat16 else 99
     rows, vocab = logits.shape
-    dev = _current()
-    assert logits.get_device() == dev and (vocab <= 1 or logits.stride(1) == 1), "the logits of a row lie side by side on the current device"
     _f32(uniform, temperature, top_p, min_p, logprob_out)
     _i32(top_k, token_out, n_kept_out)
     for t in (uniform, token_out, temperature, top_k, top_p, min_p, logprob_out, n_kept_out):
-        assert t is None or t.numel() == rows, "one entry a row"
+        if t is not None and t.numel() != rows:
+            raise AssertionError("one entry a row")
+    dev = _current()
+    if logits.get_device() != dev or (vocab > 1 and logits.stride(1) != 1):
+        raise AssertionError("the logits of a row lie side by side on the current device")
     if workspace is None:
         need = earn_sample_workspace_bytes(rows, vocab)
         workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
