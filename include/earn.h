@@ -439,7 +439,7 @@ int earn_decode_attn_beams(const earn_attn_desc* desc, const void* q, const void
  *               row's sum starts here); rows behind n are left as they are, rows from weight_rows on have no sum
  *               (where a head's softmax is NaN, as when a score is +inf or all are -inf, so is what it adds to every row that has a
  *               place; rows without one get nothing)
- *   weights_in  the same layout, or NULL (zeros); may be weights_out itself
+ *   weights_in  the same layout, or NULL (zeros); may be weights_out itself, and overlaps it in no other way
  *   out         [n_streams, Hq, d]
  *   workspace   at least earn_decode_paged_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.  The size never
  *               falls as n_streams or max_cache_len grow, or where weights are asked for: one for the largest call serves all

@@ -791,6 +791,10 @@ static int check_workspace(const char* who, size_t need, const void* workspace, 
   return EARN_OK;
 }
 
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
 int earn_cache_store(const earn_attn_desc* desc, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* start,
                      int32_t batch, int32_t total_tokens, void* k_pages, void* v_pages, const int32_t* page_table,
                      int32_t max_pages, int32_t n_pages, int32_t page_size, void* stream) {
@@ -844,6 +848,11 @@ int earn_decode_attn_paged(const earn_attn_desc* desc, const void* q, const void
   if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) { set_error("%s: q, k_new, v_new and out must be 16-byte aligned", who); return EARN_ERR_INVALID_ARG; }
   if (weights_in && !weights_out) { set_error("%s: weights_in without weights_out", who); return EARN_ERR_INVALID_ARG; }
   if (weights_out && weight_rows <= 0) { set_error("%s: weight_rows (%d) must be positive", who, weight_rows); return EARN_ERR_INVALID_ARG; }
+  const size_t w_bytes = weights_out ? (size_t)n_streams * desc->n_kv_heads * weight_rows * sizeof(float) : 0;
+  if (weights_in && weights_in != weights_out && overlap(weights_in, w_bytes, weights_out, w_bytes)) {
+    set_error("%s: weights_in and weights_out overlap without being the same", who);
+    return EARN_ERR_INVALID_ARG;
+  }
   const int forced = tuning(kTunePagedChunk, 0);   // read once: the size checked is that of the launch, whoever sets it meanwhile
   const size_t need = decode_paged_workspace_bytes(desc, n_streams, max_cache_len, weights_out != nullptr, forced);
   if ((rc = check_workspace(who, need, workspace, workspace_bytes)) != EARN_OK) return rc;
@@ -882,8 +891,12 @@ int earn_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages, c
     set_error("%s: %d new pages of %d rows do not hold budget = %d rows", who, new_max_pages, page_size, budget);
     return EARN_ERR_INVALID_ARG;
   }
-  if (weights_out == weights) { set_error("%s: weights_out must not be weights", who); return EARN_ERR_INVALID_ARG; }
   if (weights_out && weight_rows_out < budget) { set_error("%s: weight_rows_out (%d) is less than budget (%d)", who, weight_rows_out, budget); return EARN_ERR_INVALID_ARG; }
+  const size_t w_row = (size_t)n_streams * desc->n_kv_heads * sizeof(float);
+  if (weights_out && overlap(weights, w_row * weight_rows, weights_out, w_row * weight_rows_out)) {   // a sum would be overwritten before it is moved
+    set_error("%s: weights_out overlaps weights", who);
+    return EARN_ERR_INVALID_ARG;
+  }
   if ((rc = check_workspace(who, earn_cache_evict_workspace_bytes(desc, n_streams, max_cache_len, budget), workspace, workspace_bytes)) != EARN_OK) return rc;
   if (g_validate.load(std::memory_order_relaxed) && (rc = guarded(who, [&] { return validate_evict(who, cache_len, page_table, new_table, n_streams, max_cache_len, budget, max_pages, new_max_pages, n_pages, page_size, stream); })) != EARN_OK) return rc;
   return launch_cache_evict(desc, k_pages, v_pages, page_table, cache_len, n_streams, max_pages, n_pages, page_size, max_cache_len,

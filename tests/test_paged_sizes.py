@@ -108,3 +108,26 @@ def test_wrong_types_and_shapes_are_refused_without_asserts_too(flags):
     source = WRONG_KINDS if flags else WRONG_KINDS.replace("assert not assert_is_off", "pass")
     r = subprocess.run([sys.executable, *flags, "-c", source], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout + r.stderr[-2000:]
+
+
+FAKE = 1 << 20     # never dereferenced: the calls are refused
+
+
+def test_sums_that_overlap_their_source_are_refused():
+    """A call that reads sums while another of its threads writes them has no defined result, whatever part of them overlaps."""
+    import ctypes
+    desc = desc_of(B.EARN_BF16, 4, 2, 64)
+    S, rows, budget = 2, 100, 64
+    for other in (FAKE + 4, FAKE - 4, FAKE + S * 2 * rows * 4 - 4, FAKE - S * 2 * rows * 4 + 4):
+        rc = B.lib().earn_decode_attn_paged(ctypes.byref(desc), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, S, 7, 9, 16, rows, FAKE, other,
+                                            rows, FAKE, FAKE, 1 << 40, None)
+        assert rc == B.EARN_ERR_INVALID_ARG and "overlap" in B.last_error(), (rc, B.last_error())
+    # what only touches, or is the same, passes on to the next check (here: of the workspace)
+    for other in (FAKE, FAKE + S * 2 * rows * 4, FAKE - S * 2 * rows * 4):
+        rc = B.lib().earn_decode_attn_paged(ctypes.byref(desc), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, S, 7, 9, 16, rows, FAKE, other,
+                                            rows, FAKE, None, 0, None)
+        assert rc == B.EARN_ERR_WORKSPACE_TOO_SMALL, (rc, B.last_error())
+    for other in (FAKE, FAKE + 4, FAKE + S * 2 * rows * 4 - 4, FAKE - S * 2 * budget * 4 + 4):
+        rc = B.lib().earn_cache_evict(ctypes.byref(desc), FAKE, FAKE, FAKE, FAKE, S, 10, 40, 16, rows, FAKE, rows, budget, 4, 8, FAKE, 4, FAKE, FAKE,
+                                      other, budget, None, 0, None)
+        assert rc == B.EARN_ERR_INVALID_ARG and "overlap" in B.last_error(), (rc, B.last_error())
