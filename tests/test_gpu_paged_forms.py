@@ -137,3 +137,81 @@ def test_a_row_without_a_page_is_a_row_of_zeros_after_eviction(dtype, budget):
     after.kp, after.vp = after.kp.nan_to_num(0.0), after.vp.nan_to_num(0.0)      # behind the last row
     after.g_kp, after.g_vp = after.g_kp.nan_to_num(0.0), after.g_vp.nan_to_num(0.0)
     after.check(out, w_out)
+
+
+def whole_bound(case):
+    return max(max(case.lens), 0)
+
+
+def streamed_bound(case):
+    """A bound by value for which the rows would exceed 256 MB, so that the kernels that keep nothing in the caches run; the rows
+    themselves are few."""
+    per_row = 2 * case.S * case.hkv * case.d * (2 if case.dtype == BF else 4)
+    return (256 << 20) // per_row + 1
+
+
+FORMS = [
+    # dtype, hq, hkv, d, page, rows of the streams: groups up to 8 and more heads, both head sizes, split ...
+    (BF, 14, 2, 64, 16, [1500, 2999]),
+    (BF, 8, 1, 64, 8, [3000, -1, 640]),
+    (BF, 9, 1, 64, 24, [2000, 1088]),
+    (BF, 16, 1, 128, 16, [2000, 1089, 0]),
+    (BF, 9, 1, 128, 7, [1300]),
+    (BF, 20, 1, 64, 32, [1700]),                  # two workgroups for the heads of a group
+    (F32, 1, 1, 64, 16, [1300, 257]),
+    (F32, 2, 1, 64, 5, [1300]),
+    (F32, 3, 1, 64, 16, [1290]),
+    (F32, 4, 1, 128, 16, [1300, 31]),
+    (F32, 2, 1, 128, 16, [1333]),
+    (F32, 1, 1, 128, 64, [1301]),
+    (F32, 7, 1, 64, 16, [1300]),
+    (F32, 8, 1, 128, 3, [1300, 2]),
+    # ... and whole, by eight waves
+    (BF, 9, 1, 64, 16, [129, 400, 600]),
+    (BF, 16, 1, 128, 16, [300, 512]),
+    (BF, 8, 1, 64, 8, [639, 100]),
+]
+
+
+@pytest.mark.parametrize("weights", [False, True], ids=["plain", "weights"])
+@pytest.mark.parametrize("bound_of", [whole_bound, streamed_bound])
+@pytest.mark.parametrize("dtype,hq,hkv,d,page,lens", FORMS)
+def test_every_form_of_the_decode_kernels(dtype, hq, hkv, d, page, lens, bound_of, weights):
+    B = _B()
+    case = Case(dtype, hq, hkv, d, page, lens)
+    out, w_out = case.run(B, weights, bound=bound_of(case))
+    case.check(out, w_out)
+
+
+@pytest.mark.parametrize("chunk", [1, 64, 192, 2048, 100000])
+@pytest.mark.parametrize("dtype,hq,hkv,d,page,lens", [
+    (BF, 8, 2, 64, 1, [2500, 63, 64]), (BF, 16, 1, 128, 3, [2049, 0, 128]), (F32, 4, 2, 64, 1, [2100, 64]), (F32, 8, 1, 128, 16, [2048, 65])])
+def test_splits_of_any_number_of_rows(dtype, hq, hkv, d, page, lens, chunk):
+    """The fewest rows of a split, so that many are joined, and the most, whose pages of one row fill the list of page numbers."""
+    B = _B()
+    case = Case(dtype, hq, hkv, d, page, lens)
+    B.earn_set_tuning("paged_chunk", chunk)
+    try:
+        for weights in (False, True):
+            out, w_out = case.run(B, weights)
+            case.check(out, w_out)
+    finally:
+        B.earn_set_tuning("paged_chunk", 0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_workspace_for_the_largest_call_serves_smaller_ones(dtype):
+    """Sized once, with what is behind it left alone; the bound and the number of streams vary from call to call."""
+    B = _B()
+    desc = B.make_desc(dtype, 8, 1, 64)
+    need = B.earn_decode_paged_workspace_bytes(desc, 6, 40000, True)
+    whole = torch.full((need + 4096,), 255, dtype=torch.uint8, device=DEV)
+    for lens, bound in (([700] * 6, 700), ([1500, 20], 1500), ([3000], 32767), ([3000, 1, 2], 40000), ([900], 900), ([100] * 5, 639)):
+        case = Case(dtype, 8, 1, 64, 16, lens)
+        call, out, w_out = bound_call(B, case, desc, whole[:need], bound)
+        call()
+        torch.cuda.synchronize()
+        want, w_want = case.run(B, True, bound=bound)
+        case.check(want, w_want)
+        assert torch.equal(out, want) and torch.equal(w_out, w_want)
+    assert (whole[need:] == 255).all()
