@@ -106,7 +106,7 @@ struct PagedParams {
   void* out;
   float* part_o; float* part_ml;         // [streams, hq, n_splits, d], [.., 2]
   float* scores;                         // [streams, hq, score_stride], base-2 exponents; kNoRow: a row without a page
-  int n_streams, hq, hkv, w_cap, max_len, n_splits, chunk, score_stride, join_rows;
+  int hq, hkv, w_cap, max_len, n_splits, chunk, score_stride, join_rows;
   float scale_log2;
   RopeTable rope;
   HeadMap heads;
@@ -716,7 +716,7 @@ struct EvictParams {
   Pages pg;
   const int32_t* cache_len; const float* w_in; float* w_out; const int32_t* new_table;
   int32_t* kept; int32_t* len_out;
-  int n_streams, max_len, w_cap, w_out_cap, budget, first, last, new_pages;
+  int max_len, w_cap, w_out_cap, budget, first, last, new_pages;
 };
 
 // a weight as an integer of the same order: NaN below everything, zeros of either sign equal; 0 is no weight's
@@ -886,7 +886,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   constexpr int UPR = D * (int)sizeof(T) / 16;
   const int i = (int)(blockIdx.x * (256 / UPR) + threadIdx.x / UPR), unit = threadIdx.x % UPR, c = blockIdx.y, u = blockIdx.z;
-  if (blockIdx.x == 0 && c == 0 && threadIdx.x == 0 && p.len_out) {
+  if (blockIdx.x == 0 && c == 0 && threadIdx.x == 0) {
     const int n = length_of(p.cache_len, u, min(p.max_len, p.w_cap), p.pg);
     p.len_out[u] = min(n, p.budget);
   }
@@ -1018,7 +1018,7 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   p.part_o = pl.part_o ? (float*)workspace : nullptr;
   p.part_ml = (float*)((char*)workspace + pl.part_o);
   p.scores = pl.scores ? (float*)((char*)workspace + pl.part_o + pl.part_ml) : nullptr;
-  p.n_streams = n_streams; p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.max_len = max_len;
+  p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.max_len = max_len;
   p.n_splits = pl.n_splits; p.chunk = pl.chunk; p.score_stride = pl.score_stride;
   const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.f / sqrtf((float)desc->head_dim);
   p.scale_log2 = scale * 1.4426950408889634f;
@@ -1085,7 +1085,7 @@ int launch_cache_evict(const earn_attn_desc* desc, void* k_pages, void* v_pages,
   EvictParams p;
   p.pg = make_pages(k_pages, v_pages, table, max_pages, n_pages, page_size, desc->n_kv_heads);
   p.cache_len = cache_len; p.w_in = w_in; p.w_out = w_out; p.new_table = new_table; p.kept = kept; p.len_out = len_out;
-  p.n_streams = n_streams; p.max_len = max_len; p.w_cap = w_cap; p.w_out_cap = w_out_cap;
+  p.max_len = max_len; p.w_cap = w_cap; p.w_out_cap = w_out_cap;
   p.budget = budget; p.first = first; p.last = last; p.new_pages = new_pages;
   const dim3 pairs(desc->n_kv_heads, n_streams);
   if (max_len <= 4096) hipLaunchKernelGGL(evict_select_kernel<4096>, pairs, dim3(kSelectThreads), 0, stream, p);
