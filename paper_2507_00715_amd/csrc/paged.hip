@@ -90,8 +90,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restric
 // decode
 // ------------------------------------------------------------------------------------------------------------------
 // The vector form (fp32): a row is spread over d / 8 lanes, a wave takes whole rows, every lane keeps softmax states of up to 8 query
-// heads over its share of them (larger groups: a workgroup each for 8 heads, which read the rows again).  Bound by HBM, with the
-// vector ALU near it: 8 streams of 16384 rows, 32 / 8 heads of 128 (1.07 GB), 207 us, 5.2 TB/s; one of 32768 (268 MB) 63.
+// heads over its share of them (larger groups: a workgroup each for 8 heads, which read the rows again: 16 streams of 8000 rows, heads of
+// 128, 8 / 1 49 us, 16 / 1 81).  Bound by HBM, with the vector ALU near it: 8 streams of 16384 rows, 32 / 8 heads of 128 (1.07 GB), 217 us, 4.95
+// TB/s; one of 32768 (268 MB) 63.
 constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / kWave;
 constexpr int kPagedMaxChunk = 2048;   // rows of a split: its page numbers lie in LDS
 
@@ -174,11 +175,7 @@ __device__ __forceinline__ void finish_group(const PagedParams& p, long long fir
   }
 }
 
-// (fp32: two 16-byte halves)
-__device__ __forceinline__ Row8<float>::Raw streamed_row(const float* p) {
-  return Row8<float>::Raw{__builtin_nontemporal_load((const f32x4*)p), __builtin_nontemporal_load((const f32x4*)(p + 4))};
-}
-template <typename T, int D, int GQ, bool STREAMED>
+template <typename T, int D, int GQ>
 __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams p) {
   constexpr int LPK = D / 8, KPW = kWave / LPK;      // lanes per row, rows per wave instruction
   constexpr int NP = GQ >= 8 ? 2 : Row8<T>::kRowsInFlight;
@@ -275,8 +272,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
         const int at = (int)p.pg.by_page.div((unsigned)j), page = pages[at - page0];
         if (page >= 0) {
           const long long from = row_offset<D>(p.pg, page, c, j - at * p.pg.page_size);
-          kr[i] = STREAMED ? streamed_row(K + from) : Row8<T>::load_raw(K + from);
-          vr[i] = STREAMED ? streamed_row(V + from) : Row8<T>::load_raw(V + from);
+          kr[i] = Row8<T>::load_raw(K + from);
+          vr[i] = Row8<T>::load_raw(V + from);
           there[i] = true;
         }
       }
@@ -1026,9 +1023,11 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   const int rc = make_head_map(desc, &p.heads, "earn_decode_attn_paged");
   if (rc != EARN_OK) return rc;
   const bool mfma = desc->dtype == EARN_BF16;
-  // Rows that the caches in front of the memory (256 MB) cannot hold until the next step are loaded without a place there: 16 streams
-  // of 8192-32768 rows 237 -> 217 us; fp32, 8 of 16384, 217 -> 207; but 256 streams of 100-500 rows, 63 MB, 19.2 -> 19.6.
-  const bool streamed = 2ll * n_streams * p.hkv * max_len * desc->head_dim * (mfma ? 2 : 4) > (256ll << 20);
+  // bf16 rows that the caches in front of the memory (256 MB) cannot hold until the next step are loaded without a place there, whole
+  // lines at a time: 16 streams of 8192-32768 rows, 32 / 8 heads of 128, 240 -> 223 us; 32 of 4000-16000, 4 heads of 64, 72 -> 66; but 256
+  // streams of 100-500 rows, 63 MB, 22 -> 24.  An fp32 row leaves memory in halves of 16 bytes a lane, half lines, which such loads fetch
+  // twice (16 of 3000-12000, 4 heads of 128, 106 -> 131; 8 of 16384, 32 / 8 heads, which gain, 217 -> 209): always through the caches.
+  const bool streamed = mfma && 2ll * n_streams * p.hkv * max_len * desc->head_dim * 2 > (256ll << 20);
   const int gq = p.hq / p.hkv, g = paged_heads(desc), parts = paged_parts(desc);
   // Eight waves share the rows of a stream that is not split, where no other workgroup would fill the CU: us, 32 streams of 256-528
   // rows, 14 / 2 heads of 64, 11.4 -> 9.5; 8 of 500, 32 / 8 heads, 13.3 -> 11.8; 16 of 100-300 11.9 -> 11.0; but 256 of 100-500, 12 / 2 heads
@@ -1055,8 +1054,7 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
     else if constexpr (sizeof(T) == 4) {
       auto vector_launch = [&](auto heads) {
         constexpr int G = decltype(heads)::value;
-        if (streamed) hipLaunchKernelGGL((paged_decode_kernel<T, D, G, true>), grid, dim3(kPagedThreads), 0, stream, p);
-        else hipLaunchKernelGGL((paged_decode_kernel<T, D, G, false>), grid, dim3(kPagedThreads), 0, stream, p);
+        hipLaunchKernelGGL((paged_decode_kernel<T, D, G>), grid, dim3(kPagedThreads), 0, stream, p);
       };
       if (g == 1) vector_launch(std::integral_constant<int, 1>{});
       else if (g == 2) vector_launch(std::integral_constant<int, 2>{});

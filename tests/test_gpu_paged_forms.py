@@ -144,7 +144,7 @@ def whole_bound(case):
 
 
 def streamed_bound(case):
-    """A bound by value for which the rows would exceed 256 MB, so that the kernels that keep nothing in the caches run; the rows
+    """A bound by value for which the rows would exceed 256 MB, so that the bf16 kernels that keep nothing in the caches run; the rows
     themselves are few."""
     per_row = 2 * case.S * case.hkv * case.d * (2 if case.dtype == BF else 4)
     return (256 << 20) // per_row + 1
