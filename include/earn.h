@@ -99,6 +99,7 @@ int earn_set_validation(int enabled);
  *   "compact_blocks"        16 KB blocks one compaction workgroup copies (1..4)
  *   "linear_tile"           1 | 2: output tile of the projection GEMMs, 256 x 128 (1) or 256 x 256 (2); default by size
  *   "paged_chunk"           rows of a split of the decode over pages, at most 2048 (default by the number of them)
+ *                           (what earn_decode_paged_workspace_bytes gives goes with it)
  *   "linear_splits"         splits of the inner dimension when a workspace is given (default by size; 1 = none)
  */
 int earn_set_tuning(const char* key, int32_t value);

@@ -38,7 +38,7 @@ __device__ __forceinline__ int capacity_of(const Pages& pg) {   // rows that a t
 
 // ------------------------------------------------------------------------------------------------------------------
 // store: a copy, four times 16 bytes of a K and a V row per thread, all asked for before the places are looked up.  256 prompts of
-// 64-1024 rows, 2 heads of 128 (180 MB read and written): 39 us, 4.6 TB/s, of 35 that a large copy takes.  (One unit a thread 48; a
+// 64-1024 rows, 2 heads of 128 (180 MB read and written): 40 us, 4.5 TB/s, of 35 that a large copy takes.  (One unit a thread 48; a
 // search for every unit's sequence instead of one a workgroup 45.)
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kStoreUnits = 4;
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedParams
 // values pass through one swizzled LDS tile of the wave's own: they leave memory whole lines at a time, as they lie there (key
 // fragments straight from memory touch half lines, which loads that leave nothing in the caches then fetch twice).  While a
 // block is worked on, the next one's rows are on their way: each half is asked for as soon as this block's is in LDS.
-// Bound by HBM: 16 streams of 8192-32768 rows, 32 / 8 heads of 128 (1.28 GB), 216 us, 5.9 TB/s; loads of the same addresses and
+// Bound by HBM: 16 streams of 8192-32768 rows, 32 / 8 heads of 128 (1.28 GB), 218 us with the joining launch, 5.9 TB/s; loads of the same addresses and
 // nothing else take 188.  (The vector form 292; key fragments straight from memory, three waves a SIMD instead of two, 225.)
 // 16 consecutive rows have a chunk at different places: a fragment's reads meet no bank twice
 template <int D>
@@ -960,11 +960,12 @@ static PagedPlan plan_paged(const earn_attn_desc* desc, int n_streams, int max_l
   PagedPlan pl{};
   const long long pairs = (long long)n_streams * desc->n_kv_heads, rows = (long long)max_len + 1;
   // Rows of a split: what leaves a workgroup per CU (fp32, whose workgroups are lighter: two), from kMinChunk, below
-  // which a workgroup's start costs more than its rows, to kMostChunk, above which the long streams' last splits run on their own.  Up to
-  // kWholeRows rows nothing is split: the joining launch costs as much as it saves.  us, 256 / 512 / 1024 / 2048 rows: 8 streams of 2000 rows, 32
-  // / 32 heads 65 / 61 / 60 / 58; 4 of 8192, 32 / 8 heads 37 / 35 / 29 / 36; one of 4096 14 / 16 / 22 / 34; 16 of 8192-32768 270 / 228 / 214
-  // / 212; one of 65521, 12 / 2 heads 26 / 24 / 27 / 39; one of 32768, fp32 74 / 64 / 70 / 118; 32 of 256-528, 14 / 2 heads of 64 12.2 / 14.4 /
-  // 11.5 whole; 256 of 100-500, 12 / 2 heads 29 / 20 whole.
+  // which a workgroup's start costs more than its rows, to kMostChunk, above which the long streams' last splits run on their own (1088: a
+  // cache of 1024 rows and its new row are one split).  Up to kWholeRows rows nothing is split: the joining launch costs as much as it
+  // saves.  us, 256 / 512 / 1024 / 1088 / 2048 rows: 8 streams of 2000 rows, 32 / 32 heads 61 / 58 / 56 / 58 / 53; 4 of 8192, 32 / 8 heads
+  // 40 / 38 / 33 / 34 / 42; one of 4096 14 / 17 / 24 / 26 / 40; 16 of 8192-32768 256 / 212 / 201 / 202 / 199; 64 of 1024, 8 / 8 heads 68 / 65
+  // / 63 / 56 / 57; one of 65521, 12 / 2 heads, weights 26 / 24 / 30 / 31 / 46; one of 32768, fp32 72 / 63 / 71 / 73 / 119; 32 of 256-528, 14 / 2
+  // heads of 64 11.6 / 14.4 / 10.1 whole; 256 of 100-500, 12 / 2 heads 29 / 21 whole.
   long long chunk = rows * pairs / wanted_workgroups(desc);
   if (chunk < kMinChunk) chunk = kMinChunk;
   if (chunk > kMostChunk) chunk = kMostChunk;
@@ -1030,8 +1031,8 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
   const bool streamed = mfma && 2ll * n_streams * p.hkv * max_len * desc->head_dim * 2 > (256ll << 20);
   const int gq = p.hq / p.hkv, g = paged_heads(desc), parts = paged_parts(desc);
   // Eight waves share the rows of a stream that is not split, where no other workgroup would fill the CU: us, 32 streams of 256-528
-  // rows, 14 / 2 heads of 64, 11.4 -> 9.5; 8 of 500, 32 / 8 heads, 13.3 -> 11.8; 16 of 100-300 11.9 -> 11.0; but 256 of 100-500, 12 / 2 heads
-  // (512 workgroups), 20.3 -> 25.4, and split caches gain nothing (one of 65521 rows 24.3 -> 25.7).
+  // rows, 14 / 2 heads of 64, 13.3 -> 11.7; 8 of 500, 32 / 8 heads, 16.0 -> 13.3; 16 of 100-300, 12 / 2 heads, 13.7 -> 12.5; but 256 of 100-500, 12 / 2
+  // heads (512 workgroups), 22 -> 27, and split caches gain nothing (one of 65521 rows 24.3 -> 25.7).
   const bool wide = pl.n_splits == 1 && (long long)p.hkv * parts * n_streams <= 256 && pl.chunk > 128;
   // splits last: consecutive workgroups go to the XCDs in turn, and with two splits side by side every other XCD had short ones only
   // (64 streams of 256-2080 rows, 32 heads, two splits: 277 us, this way 209)
@@ -1066,7 +1067,7 @@ int launch_decode_paged(const earn_attn_desc* desc, const void* q, const void* k
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
     {
-      // rows of a block: 1024, more where the blocks are many (64 streams of up to 2080 rows, 32 heads: 16 -> 11 us)
+      // rows of a block: 1024, more where the blocks are many (64 streams of up to 2080 rows, 32 heads: 16 -> 12 us)
       const long long blocks = ((long long)max_len + kWeightRows) / kWeightRows, more = blocks * p.hkv * n_streams / 2048;
       p.join_rows = kWeightRows * (int)(more < 1 ? 1 : more > 8 ? 8 : more);
       const int row_blocks = w_out ? (int)(((long long)max_len + p.join_rows) / p.join_rows) : 0;

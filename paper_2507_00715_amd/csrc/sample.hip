@@ -17,8 +17,8 @@
 //   - top-k up to kSmallK: the largest entries of every 16 bytes (of longer rows, of some of them together) stay in LDS; a histogram of
 //     them over (l_max - l) / T gives a border that at least k entries reach, and few more: those are listed, and the rest happens in the
 //     list;
-//   - else top-k: a histogram of all entries; top-p: one of their weights; the few entries of the bin in which a beginning ends are
-//     ranked among each other;
+//   - else top-k: a histogram of all entries; top-p: one of their weights; the entries of the bin in which a beginning ends are
+//     ranked among each other, or found bit by bit where they are more than the list holds;
 //   - the kept weights' sums by wave (gathered 64 at a time before their exponentials are taken, where few of the entries are kept;
 //     with top-p in the same pass that lists the bin's), then by unit of the wave that u W falls to, all waves together.
 #include <type_traits>
@@ -271,7 +271,9 @@ __device__ __forceinline__ void find_equal(const R& run, float value, int r, Sam
 }
 
 // The beginning that the k-th entry ends, or the first entry at which the weights reach `mass`, of those in `within`, where the bin that
-// it ends in holds too many for the list (mostly equal logits): the last key, bit by bit, then its equals in order of their index.
+// it ends in, T / 64 wide, holds too many for the list: equal logits, flat rows, and large vocabularies at ordinary temperatures.  The last
+// key, bit by bit, 33 passes over the row, then its equals in order of their index.  131072 normal logits, top-p 0.9: 731 us where their
+// deviation is half of T, 74 where it is 2.5 T and the list holds them; 40000 equal ones 239-270 us.
 // Called by all threads.
 template <bool BY_MASS, typename R, int WAVES>
 __device__ __forceinline__ Beginning find_bit_by_bit(const R& run, const Weights& wt, const Beginning& within, int bin, int before, u64 mass_before, int k,
